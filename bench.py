@@ -45,9 +45,11 @@ BOUND = {"tiny": "hbm", "llama3_8b": "hbm", "prefill_heavy": "mfma", "decode_hea
 # HBM bytes per launch of the main attention kernel from rocprofv3 --pmc FETCH_SIZE / WRITE_SIZE
 # runs of this file, scaled by what the same counters read for a plain 1 GiB copy (FETCH_SIZE x
 # 2.000, WRITE_SIZE x 1.000).  These are STATIC figures copied from the summary named below, taken
-# with the library version named below; with any other library version the line carries null.
+# with the library version named below; with any other library version the line carries null (the versions
+# that only added entry points since are listed: the attention kernel's code is the same).
 TRAFFIC_SOURCE = "profiles/attn_mixed_kernel_benchmark_batches_rocprofv3.md"
 TRAFFIC_LIB_VERSION = 511
+SAME_ATTENTION_AS_TRAFFIC = (511, 600)
 MEASURED_TRAFFIC_BYTES = {"llama3_8b": 616036662, "prefill_heavy": 592820473, "decode_heavy": 4876803129,
                           "llama_70b_fp8": 4021260357, "paper_iteration_16k": 301404885}
 
@@ -131,7 +133,7 @@ def time_workload(name, steps, warmup, trial=0):
     rate = lambda ms: work / (ms * 1e-3)
     sh = batch.shape
     append_bytes = (it.n_prefix_tokens + it.n_new_tokens) * sh.n_kv_heads * sh.head_dim * 2 * (2 + (1 if it.fp8 else 2))
-    traffic = MEASURED_TRAFFIC_BYTES.get(name) if B.version() == TRAFFIC_LIB_VERSION else None
+    traffic = MEASURED_TRAFFIC_BYTES.get(name) if B.version() in SAME_ATTENTION_AS_TRAFFIC else None
     span_mean, main_mean = float(span_ms.mean()), float(main_ms.mean())
     res = {
         "workload": name,

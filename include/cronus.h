@@ -10,7 +10,7 @@
  * terms: continuation chunk against its prefill context, decodes against their
  * contexts).  The cache is managed in blocks of N_size tokens (Algorithm 1).
  *
- * Two operations:
+ * Two operations (and, for loops that draft tokens, three more: "Drafted tokens" below):
  *   cronus_kv_append  - place K/V rows (a transferred prefix, or this iteration's new
  *                       tokens) into paged blocks through a block table.
  *   cronus_attn_mixed - causal attention of every sequence's chunk rows against
@@ -67,7 +67,7 @@ typedef enum {
   CRONUS_OK = 0,
   CRONUS_ERR_INVALID_ARG = 1, /* null pointer, negative size, lengths that do not fit the table */
   CRONUS_ERR_UNSUPPORTED = 2, /* head_dim not 64/128, block_size != 16, Hq % Hkv != 0, unknown dtype */
-  CRONUS_ERR_WORKSPACE = 3,   /* workspace smaller than cronus_attn_mixed_workspace_bytes() */
+  CRONUS_ERR_WORKSPACE = 3,   /* workspace smaller than cronus_attn_mixed_workspace_bytes() (cronus_attn_tree: its own) */
   CRONUS_ERR_HIP = 4          /* a HIP runtime call failed */
 } cronus_status;
 
@@ -101,7 +101,7 @@ typedef struct cronus_kv_cache {
  *   cu_tokens    : device, int32 [n_seqs+1], exclusive prefix sums, cu_tokens[0] = 0
  *   start_pos    : device, int32 [n_seqs]
  *   block_tables : device, int32 [n_seqs][max_blocks_per_seq]
- *   n_tokens     : total rows (= cu_tokens[n_seqs]); 0 is a no-op
+ *   n_tokens     : total rows (= cu_tokens[n_seqs], or more where only the device knows that: it sizes the launch); 0 is a no-op
  * Only the addressed slots are written.  The copy is bit-exact for bf16.
  * Errors: INVALID_ARG (null pointer, negative count), UNSUPPORTED (shape/dtype).
  */
@@ -272,6 +272,108 @@ int cronus_kv_gather(const cronus_kv_cache* cache, void* k_dst, void* v_dst,
                      const int32_t* cu_tokens, const int32_t* start_pos,
                      const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t n_seqs,
                      int32_t n_tokens, void* hip_stream);
+
+/*
+ * Drafted tokens.  A serving loop that drafts tokens and verifies them as a tree does not know on the host how long its
+ * sequences are after an iteration.  The three entry points below take all lengths from device memory, so that iterations
+ * follow one another, and are captured into a HIP graph, with no word from the host:
+ *   cronus_build_tables -> cronus_kv_append of the drafted rows, cronus_attn_tree (per layer) -> the caller's choice of a
+ *   path -> cronus_kv_commit -> the next cronus_build_tables, whose kv_lens are cronus_kv_commit's kv_lens_out.
+ * They allocate nothing and keep nothing between calls.  Lengths are checked on the device, where they are; what a call
+ * does about lengths that do not fit is said with each.  Pointers and sizes are checked on the host.
+ */
+
+/* What cronus_build_tables reports in report[0]. */
+typedef enum {
+  CRONUS_TABLES_OK = 0,
+  CRONUS_TABLES_BAD_LENGTHS = 1,    /* report[3]: the first such sequence, or -1: the free list itself (count or capacity) */
+  CRONUS_TABLES_NO_BLOCKS = 2,      /* more blocks needed than the free list has */
+  CRONUS_TABLES_TOO_MANY_TOKENS = 3 /* more new tokens than max_tokens */
+} cronus_tables_status;
+
+typedef struct cronus_paged_tables {
+  int32_t* block_tables;     /* device, [n_seqs][max_blocks_per_seq]; entries [0, held) of a row are its blocks  */
+  int32_t max_blocks_per_seq;
+  const int32_t* held;       /* device, [n_seqs]: blocks that each sequence has                                  */
+  int32_t* held_out;         /* device, [n_seqs]: those that it has afterwards; may be held                      */
+  int32_t* free_blocks;      /* device, [free_capacity]: a stack of free block ids, entries [0, count)           */
+  int32_t free_capacity;
+  const int32_t* free_count; /* device, [1]: count                                                               */
+  int32_t* free_count_out;   /* device, [1]: count afterwards; may be free_count                                 */
+} cronus_paged_tables;
+
+/*
+ * cronus_build_tables - block tables, row offsets and the cache slot of every new token, from lengths on the device
+ * (blocks of N_size tokens, Algorithm 1).  Sequence s has kv_lens[s] tokens cached and gets new_lens[s] >= 0 more, or has
+ * ended (new_lens[s] = -1: it gets none, and its held blocks go on top of the free stack, in the order of the sequences and of
+ * the entries of a row).  Then every sequence is granted what it lacks,
+ *     need[s] = max(0, ceil((kv_lens[s] + new_lens[s]) / 16) - held[s]),
+ * behind its held blocks: the i-th block granted in the batch (sequences in order) is the i-th from the top of the stack.  Blocks
+ * that rejected drafts no longer use stay held.
+ *   cu_tokens : device, int32 [n_seqs+1], out: exclusive prefix sums of the new tokens (ended: 0)
+ *   start_pos : device, int32 [n_seqs], out: kv_lens[s]; 0 for an ended sequence
+ *   cu_blocks : device, int32 [n_seqs+1], out: exclusive prefix sums of need
+ *   slot_map  : device, int64 [max_tokens] or NULL, out: block * 16 + slot of new token i of sequence s at cu_tokens[s] + i;
+ *               entries behind the last token are left as they were
+ *   max_tokens: most new tokens of the batch (sizes the launch; a loop of fixed tree sizes knows it)
+ *   report    : device, int32 [4], out: cronus_tables_status, new tokens, blocks granted, sequence (see the enum)
+ * cu_tokens and start_pos are what cronus_kv_append, cronus_kv_gather, cronus_attn_tree and cronus_kv_commit take.
+ * All or nothing: where lengths do not fit (negative; held < ceil(kv_lens / 16); more than max_blocks_per_seq blocks; an ended
+ * sequence's included), the blocks do not suffice or there are more than max_tokens tokens, report[0] says so, report[1] and [2] hold what
+ * was asked for (0 lengths aside), block_tables, free_blocks, held and the count stay as they were, cu_tokens and cu_blocks are all 0 and start_pos is kv_lens: the
+ * calls that take them then do nothing.
+ * Outputs must not overlap inputs or one another, but for the pairs named above.
+ * Errors: INVALID_ARG (null pointer, negative size), HIP.
+ */
+int cronus_build_tables(const cronus_paged_tables* tables, const int32_t* kv_lens, const int32_t* new_lens, int32_t n_seqs,
+                        int32_t* cu_tokens, int32_t* start_pos, int32_t* cu_blocks, int64_t* slot_map, int32_t max_tokens,
+                        int32_t* report, void* hip_stream);
+
+/*
+ * cronus_attn_tree - attention of drafted tokens over the paged cache.  Sequence s has n = cu_rows[s+1] - cu_rows[s] drafted
+ * tokens; token i is row cu_rows[s] + i of q and out, its K/V lie at position prefix_lens[s] + i (cronus_kv_append).  It attends
+ * to all positions before prefix_lens[s], and to position prefix_lens[s] + j, j < n, where bit j % 64 of word j / 64 of its row of the mask
+ * is set (its ancestors and itself, in a tree).  Same products, statistics and rounding as cronus_attn_mixed.
+ *   q, out       : device, bf16 [rows][Hq][D], at any address of a bf16 element
+ *   prefix_lens  : device, int32 [n_seqs]
+ *   cu_rows      : device, int32 [n_seqs+1], rising
+ *   mask         : device, uint64 [rows][mask_words] (8-byte aligned), or NULL: token i sees j <= i (drafts in a chain; n = 1:
+ *                  an ordinary decode).  Bits from n on are not looked at.  A row that sees no key at all gets zeros
+ *   mask_words   : words of a mask row, at least ceil(max_rows / 64); not looked at without a mask
+ *   max_rows     : most drafted tokens of a sequence (chooses the kernel)
+ *   workspace    : device, at least cronus_attn_tree_workspace_bytes(cache, max_rows) bytes, 256-byte aligned; contents as for
+ *                  cronus_attn_mixed, and not to be shared by calls that can overlap
+ * Infinite and NaN K or V of a drafted token reach the rows that see it and no others; slots behind the last drafted token are not used.
+ * A sequence with n <= 0 or n > max_rows, a negative prefix or more than 16 * max_blocks_per_seq (or 2^31 - 256) positions is
+ * passed over: its rows of out are left as they were, as are rows outside of all sequences.
+ * The results of a call depend on its arguments alone (no atomics), and on the number of CUs.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ */
+int cronus_attn_tree(const cronus_kv_cache* cache, const void* q, void* out, const int32_t* prefix_lens, const int32_t* cu_rows,
+                     const uint64_t* mask, int32_t mask_words, const int32_t* block_tables, int32_t max_blocks_per_seq,
+                     int32_t n_seqs, int32_t max_rows, float sm_scale, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Bytes of workspace cronus_attn_tree needs; 0 on invalid arguments.  Does not depend on the sequences or their lengths; larger max_rows
+ * need at least as much. */
+size_t cronus_attn_tree_workspace_bytes(const cronus_kv_cache* cache, int32_t max_rows);
+
+/*
+ * cronus_kv_commit - keep the accepted drafted tokens.  In every one of n_caches caches (a model's layers: same heads, head_dim
+ * and dtype, same block tables) the K/V of sequence s at position start_pos[s] + paths[s][k] move to start_pos[s] + k, for
+ * k = 0 .. m - 1 in effect at once, and kv_lens_out[s] = start_pos[s] + m.
+ *   caches      : host, cronus_kv_cache [n_caches]
+ *   start_pos   : device, int32 [n_seqs]; cu_rows: device, int32 [n_seqs+1], the drafted tokens as for cronus_attn_tree
+ *   paths       : device, int32 [n_seqs][max_path], accepted tokens, strictly rising (a token lies behind its parent); path_lens:
+ *                 device, int32 [n_seqs].  A path ends early (m < path_lens[s]) at max_path and at the first entry that is not one of
+ *                 the sequence's tokens or not behind the entry before it
+ *   kv_lens_out : device, int32 [n_seqs], or NULL; must not overlap start_pos, cu_rows, paths or path_lens
+ * m = 0 for a sequence whose drafted tokens do not lie in [0, 16 * max_blocks_per_seq).  The blocks from start_pos[s] on must
+ * not be shared by sequences.  Bits move unchanged; all other slots keep theirs.
+ * Errors: INVALID_ARG (also: caches that differ, kv_lens_out overlaps start_pos), UNSUPPORTED, HIP.
+ */
+int cronus_kv_commit(const cronus_kv_cache* caches, int32_t n_caches, const int32_t* start_pos, const int32_t* cu_rows,
+                     const int32_t* paths, int32_t max_path, const int32_t* path_lens, const int32_t* block_tables,
+                     int32_t max_blocks_per_seq, int32_t n_seqs, int32_t* kv_lens_out, void* hip_stream);
 
 /*
  * Execution-time models that the balancer uses (section 4.4): a partial prefill of L

@@ -22,10 +22,15 @@ CRONUS_ERR_WORKSPACE = 3
 CRONUS_ERR_HIP = 4
 CRONUS_KV_BF16 = 0
 CRONUS_KV_FP8_E4M3 = 1
+CRONUS_TABLES_OK = 0
+CRONUS_TABLES_BAD_LENGTHS = 1
+CRONUS_TABLES_NO_BLOCKS = 2
+CRONUS_TABLES_TOO_MANY_TOKENS = 3
 
 EXPORTS = ("cronus_kv_append", "cronus_kv_append_pair", "cronus_kv_gather", "cronus_attn_mixed", "cronus_iteration", "cronus_attn_mixed_static",
            "cronus_attn_mixed_workspace_bytes",
-           "cronus_attn_mixed_plan_stats", "cronus_attn_mixed_plan_items", "cronus_balancer_split",
+           "cronus_attn_mixed_plan_stats", "cronus_attn_mixed_plan_items", "cronus_build_tables", "cronus_attn_tree",
+           "cronus_attn_tree_workspace_bytes", "cronus_kv_commit", "cronus_balancer_split",
            "cronus_profile_events", "cronus_probe_mfma", "cronus_probe_mfma_16x16x32", "cronus_probe_mfma_sink_floats", "cronus_status_string",
            "cronus_version")
 
@@ -48,6 +53,12 @@ class cronus_balancer_model(ctypes.Structure):
 class cronus_kv_rows(ctypes.Structure):
     _fields_ = [("k_src", ctypes.c_void_p), ("v_src", ctypes.c_void_p), ("cu_tokens", ctypes.c_void_p),
                 ("start_pos", ctypes.c_void_p), ("n_tokens", ctypes.c_int32)]
+
+
+class cronus_paged_tables(ctypes.Structure):
+    _fields_ = [("block_tables", ctypes.c_void_p), ("max_blocks_per_seq", ctypes.c_int32), ("held", ctypes.c_void_p),
+                ("held_out", ctypes.c_void_p), ("free_blocks", ctypes.c_void_p), ("free_capacity", ctypes.c_int32),
+                ("free_count", ctypes.c_void_p), ("free_count_out", ctypes.c_void_p)]
 
 
 class CronusError(RuntimeError):
@@ -92,6 +103,14 @@ def lib() -> ctypes.CDLL:
         L.cronus_attn_mixed_plan_stats.restype = ctypes.c_int
         L.cronus_attn_mixed_plan_items.argtypes = [cp, i32p, i32p, i32, i32p, ctypes.c_int64]
         L.cronus_attn_mixed_plan_items.restype = ctypes.c_int64
+        L.cronus_build_tables.argtypes = [ctypes.POINTER(cronus_paged_tables), vp, vp, i32, vp, vp, vp, vp, i32, vp, vp]
+        L.cronus_build_tables.restype = ctypes.c_int
+        L.cronus_attn_tree.argtypes = [cp, vp, vp, vp, vp, vp, i32, vp, i32, i32, i32, ctypes.c_float, vp, ctypes.c_size_t, vp]
+        L.cronus_attn_tree.restype = ctypes.c_int
+        L.cronus_attn_tree_workspace_bytes.argtypes = [cp, i32]
+        L.cronus_attn_tree_workspace_bytes.restype = ctypes.c_size_t
+        L.cronus_kv_commit.argtypes = [cp, i32, vp, vp, vp, i32, vp, vp, i32, i32, vp, vp]
+        L.cronus_kv_commit.restype = ctypes.c_int
         L.cronus_profile_events.argtypes = [vp, vp, vp, vp]
         L.cronus_profile_events.restype = None
         for probe in (L.cronus_probe_mfma, L.cronus_probe_mfma_16x16x32):
@@ -346,4 +365,49 @@ def cronus_attn_mixed_static(cache: cronus_kv_cache, q, out, prefix_lens, chunk_
                                         stream)
     if check and rc != CRONUS_OK:
         raise CronusError(rc, "cronus_attn_mixed_static")
+    return rc
+
+
+def cronus_build_tables(tables, kv_lens, new_lens, n_seqs: int, cu_tokens, start_pos, cu_blocks, slot_map, max_tokens: int, report,
+                        stream: int = 0, check=True) -> int:
+    """tables: (block_tables, max_blocks_per_seq, held, held_out, free_blocks, free_capacity, free_count, free_count_out); these and
+    the others: device tensors (or addresses).  What the device finds wrong with the lengths is in report, not in the status."""
+    bt, width, held, held_out, free, capacity, count, count_out = tables
+    t = cronus_paged_tables(_ptr(bt), int(width), _ptr(held), _ptr(held_out), _ptr(free), int(capacity), _ptr(count), _ptr(count_out))
+    rc = lib().cronus_build_tables(ctypes.byref(t), _ptr(kv_lens), _ptr(new_lens), int(n_seqs), _ptr(cu_tokens), _ptr(start_pos),
+                                   _ptr(cu_blocks), _ptr(slot_map), int(max_tokens), _ptr(report), stream)
+    if check and rc != CRONUS_OK:
+        raise CronusError(rc, "cronus_build_tables")
+    return rc
+
+
+def cronus_attn_tree_workspace_bytes(cache: cronus_kv_cache, max_rows: int) -> int:
+    return int(lib().cronus_attn_tree_workspace_bytes(ctypes.byref(cache), int(max_rows)))
+
+
+def cronus_attn_tree(cache: cronus_kv_cache, q, out, prefix_lens, cu_rows, mask, mask_words: int, block_tables,
+                     max_blocks_per_seq: int, n_seqs: int, max_rows: int, sm_scale: float, workspace, workspace_bytes: int,
+                     stream: int = 0, check=True) -> int:
+    """All arrays: device tensors (or addresses); mask: uint64 words (an int64 tensor will do), or None for a chain."""
+    rc = lib().cronus_attn_tree(ctypes.byref(cache), _ptr(q), _ptr(out), _ptr(prefix_lens), _ptr(cu_rows), _ptr(mask), int(mask_words),
+                                _ptr(block_tables), int(max_blocks_per_seq), int(n_seqs), int(max_rows), float(sm_scale),
+                                _ptr(workspace), int(workspace_bytes), stream)
+    if check and rc != CRONUS_OK:
+        raise CronusError(rc, "cronus_attn_tree")
+    return rc
+
+
+def cache_array(caches):
+    """The caches of a model's layers as cronus_kv_commit takes them (a loop makes the array once)."""
+    return caches if isinstance(caches, ctypes.Array) else (cronus_kv_cache * len(caches))(*caches)
+
+
+def cronus_kv_commit(caches, start_pos, cu_rows, paths, max_path: int, path_lens, block_tables, max_blocks_per_seq: int, n_seqs: int,
+                     kv_lens_out, stream: int = 0, check=True) -> int:
+    """caches: cronus_kv_cache of every layer (a list, or cache_array() of it); the others: device tensors (or addresses)."""
+    array = cache_array(caches)
+    rc = lib().cronus_kv_commit(array, len(array), _ptr(start_pos), _ptr(cu_rows), _ptr(paths), int(max_path), _ptr(path_lens),
+                                _ptr(block_tables), int(max_blocks_per_seq), int(n_seqs), _ptr(kv_lens_out), stream)
+    if check and rc != CRONUS_OK:
+        raise CronusError(rc, "cronus_kv_commit")
     return rc

@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcronus.so")
-SOURCES = ["api.cpp", "plan.cpp", "balancer.cpp", "kv_append.hip", "kv_gather.hip", "attn_mixed.hip", "mfma_probe.hip"]
+SOURCES = ["api.cpp", "api_draft.cpp", "plan.cpp", "balancer.cpp", "kv_append.hip", "kv_gather.hip", "attn_mixed.hip", "build_tables.hip",
+           "attn_tree.hip", "kv_commit.hip", "mfma_probe.hip"]
 # Loops on cache lines: the steady loop of the chunk tiles takes up to 1 % more or less with its place in memory
 # (attention of 28 k-key fp8 chunks 5.93 ms at one place, 5.98 at another; 5.94 aligned).
 FLAGS = ["--offload-arch=gfx950", "-O3", "-falign-loops=64", "-std=c++17", "-fPIC", "-shared", "-Xclang", "-target-feature", "-Xclang",

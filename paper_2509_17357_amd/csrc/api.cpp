@@ -8,37 +8,12 @@
 #include <mutex>
 #include <vector>
 
+#include "api_checks.h"
 #include "cronus_internal.h"
 #include "plan_ring.h"
 
 namespace cronus {
 namespace {
-
-int check_cache(const cronus_kv_cache* c) {
-  if (!c || !c->k_cache || !c->v_cache || c->num_blocks <= 0) return CRONUS_ERR_INVALID_ARG;
-  if (c->num_q_heads <= 0 || c->num_kv_heads <= 0) return CRONUS_ERR_INVALID_ARG;
-  if (c->block_size != kBlock) return CRONUS_ERR_UNSUPPORTED;
-  if (c->head_dim != 64 && c->head_dim != 128) return CRONUS_ERR_UNSUPPORTED;
-  if (c->num_q_heads % c->num_kv_heads) return CRONUS_ERR_UNSUPPORTED;
-  if (c->kv_dtype == CRONUS_KV_BF16) {
-    if (c->k_scale || c->v_scale) return CRONUS_ERR_INVALID_ARG;
-  } else if (c->kv_dtype == CRONUS_KV_FP8_E4M3) {
-    if (!c->k_scale || !c->v_scale) return CRONUS_ERR_INVALID_ARG;
-  } else {
-    return CRONUS_ERR_UNSUPPORTED;
-  }
-  return CRONUS_OK;
-}
-
-// Shape-only variant for the size queries, which need no device pointers.
-int check_shape(const cronus_kv_cache* c) {
-  if (!c || c->num_q_heads <= 0 || c->num_kv_heads <= 0) return CRONUS_ERR_INVALID_ARG;
-  if (c->block_size != kBlock) return CRONUS_ERR_UNSUPPORTED;
-  if (c->head_dim != 64 && c->head_dim != 128) return CRONUS_ERR_UNSUPPORTED;
-  if (c->num_q_heads % c->num_kv_heads) return CRONUS_ERR_UNSUPPORTED;
-  if (c->kv_dtype != CRONUS_KV_BF16 && c->kv_dtype != CRONUS_KV_FP8_E4M3) return CRONUS_ERR_UNSUPPORTED;
-  return CRONUS_OK;
-}
 
 // Per-device facts and one-time set-up, guarded by g_mu.  Index = HIP device ordinal.
 struct DeviceState {
@@ -51,7 +26,8 @@ constexpr int kMaxDevices = 64;
 DeviceState g_dev[kMaxDevices];
 std::mutex g_mu;
 
-// CU count of the current device; 256 (MI355X) when sizes are queried without a device.
+}  // namespace
+
 int device_cus() {
   int dev = 0, n = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
@@ -67,6 +43,8 @@ int device_cus() {
   g_dev[dev].n_cus = n;
   return n;
 }
+
+namespace {
 
 // Set-up that must precede the first launch on the current device (kernel attributes).
 // Caller holds g_mu.
@@ -295,8 +273,6 @@ bool read_from(const cronus_kv_cache* cache, const cronus_kv_rows* rows, int32_t
   return meets(rows->k_src, values) || meets(rows->v_src, values) || meets(rows->cu_tokens, ints + sizeof(int32_t)) || meets(rows->start_pos, ints);
 }
 
-bool workspace_refused(const void* workspace) { return !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u); }
-
 // cronus_attn_mixed behind the placing of the rows of `first` and `second` (null: none).
 int attn_mixed(const cronus_kv_cache* cache, const cronus_kv_rows* first, const cronus_kv_rows* second, const void* q, void* out,
                const int32_t* prefix_lens, const int32_t* chunk_lens, const int32_t* block_tables, int32_t max_blocks_per_seq,
@@ -483,6 +459,6 @@ const char* cronus_status_string(int status) {
   }
 }
 
-int cronus_version(void) { return 511; }  // 0.5.11: decode iterations place their rows in the attention launch only where that is faster and the rows do not lie in what it writes
+int cronus_version(void) { return 600; }  // 0.6.0: drafted tokens: cronus_build_tables, cronus_attn_tree, cronus_kv_commit
 
 }  // extern "C"

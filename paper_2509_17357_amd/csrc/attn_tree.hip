@@ -1,0 +1,504 @@
+// Attention of drafted tokens over a paged cache, lengths on the device.  Row i of sequence s (one of its n drafted tokens, K/V at
+// position L + i) attends to the L cached keys and to the drafted ones that bit j of its mask names:
+//     out_i = sum_j w_ij V_j / sum_j w_ij,  w_ij = exp(scale <q_i, K_j> - m_i),  j < L or (j = L + k, k < n, bit k of mask_i).
+//
+// The host does not know the lengths, so a launch has as many work-groups as the GPU has CUs, and each finds its share itself: the
+// batch is a sequence of U units (a row tile of a KV head against kUnitKeys keys; keys run fastest, then row tiles, heads, sequences),
+// and share l of A = min(work-groups, U) is units [l U / A, (l + 1) U / A), at least one.  Neighbouring shares, whose row tiles read the same
+// keys, go to one XCD.  A row tile whose units lie in several shares is left as partial results (m, l, O), which
+// merge_kernel combines; a share has at most two of them, one at either end, so the workspace does not depend on the lengths.
+//
+// Eight wavefronts: WR of them side by side hold 32 rows each (a row is a drafted token and a query head of the KV head), and
+// 8 / WR such groups take every (8 / WR)-th 32-key sub-tile.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: a row is a
+// column, its lanes are l and l + 32, P stays in registers, and the operands are the cache's own 16-byte chunks (8 bytes, fp8), loaded
+// straight into registers.
+#include <hip/hip_runtime.h>
+
+#include "cronus_internal.h"
+#include "lane_ops.h"
+
+namespace cronus {
+namespace {
+
+constexpr int kUnitKeys = 64;
+
+struct TreeParams {
+  const unsigned short* q;
+  unsigned short* out;
+  const unsigned char* k_pool;
+  const unsigned char* v_pool;
+  const float* k_scale;
+  const float* v_scale;
+  const int* prefix_lens;
+  const int* cu_rows;
+  const unsigned long long* mask;  // or nullptr: a chain
+  const int* block_tables;
+  float* partials;        // two slots a work-group
+  struct Split* splits;   // one a work-group
+  int mask_words, max_blocks, n_seqs, max_rows, n_q_heads, n_kv_heads;
+  float scale_log2e;
+};
+
+// A row tile whose units lie in the shares of several work-groups, left by the one that has its first unit: the pieces are that one's
+// slot 1 and slot 0 of the next n_pieces - 1.
+struct Split {
+  int n_pieces;  // 0: none
+  int share;     // that work-group's share
+  int n_rows;    // rows of the tile
+  int row0;      // first of them among the sequence's rows of this KV head
+  int kv_head;
+  int first_token;  // cu_rows of the sequence
+  int prefix, count;
+};
+static_assert(sizeof(Split) == 32);
+
+// Floats of a slot: O, then (m in log2 units, l) of every row.
+template <int D, int WR> constexpr int kSlotFloats = 32 * WR * (D + 2);
+
+// The sequence's lengths, or no rows where they are none that this call could serve.
+struct Lens {
+  int prefix, count, first;
+};
+__device__ __forceinline__ Lens lens_of(const TreeParams& p, int s) {
+  const int first = p.cu_rows[s], next = p.cu_rows[s + 1], prefix = p.prefix_lens[s];
+  const long long count = (long long)next - first;
+  const bool good = first >= 0 && count > 0 && count <= p.max_rows && prefix >= 0 &&
+                    prefix + count <= min((long long)p.max_blocks * kBlock, kTreeMostKeys);
+  return good ? Lens{prefix, (int)count, first} : Lens{0, 0, 0};
+}
+template <int WR>
+__device__ __forceinline__ int row_tiles(const TreeParams& p, const Lens& n) {
+  return (n.count * (p.n_q_heads / p.n_kv_heads) + 32 * WR - 1) / (32 * WR);
+}
+__device__ __forceinline__ int key_units(const Lens& n) { return (n.prefix + n.count + kUnitKeys - 1) / kUnitKeys; }
+
+// 32 bits: which of the keys first_key .. first_key + 31 the row of drafted token `token` sees.
+__device__ __forceinline__ unsigned visible_bits(const TreeParams& p, const Lens& n, int token, int first_key) {
+  const int at = first_key - n.prefix;  // of the first key, among the drafted tokens
+  if (at >= n.count) return 0;
+  if (at <= -32) return ~0u;
+  unsigned bits;
+  if (!p.mask) {
+    const int seen = token + 1 - at;  // keys of the 32 before the first that it does not see
+    bits = seen >= 32 ? ~0u : seen > 0 ? (1u << seen) - 1 : 0;
+  } else {
+    const unsigned long long* row = p.mask + (long long)(n.first + token) * p.mask_words;
+    if (at < 0) {
+      bits = (unsigned)(row[0] << -at) | ((1u << -at) - 1);
+    } else {
+      const int w = at >> 6, shift = at & 63;
+      unsigned long long x = row[w] >> shift;
+      if (shift > 32 && w + 1 < p.mask_words) x |= row[w + 1] << (64 - shift);
+      bits = (unsigned)x;
+    }
+  }
+  const int left = n.count - at;
+  return left >= 32 ? bits : bits & ((1u << left) - 1);
+}
+// Whether the row sees nothing: its output is 0 then (and not the quotient of two zeros).
+__device__ bool sees_nothing(const TreeParams& p, const Lens& n, int token) {
+  if (n.prefix > 0) return false;
+  for (int at = 0; at < n.count; at += 32)
+    if (visible_bits(p, n, token, at)) return false;
+  return true;
+}
+
+__device__ __forceinline__ bool not_finite(u32x4 v) {
+  bool found = false;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) found |= (v[w] & 0x7f80u) == 0x7f80u || (v[w] & 0x7f800000u) == 0x7f800000u;
+  return found;
+}
+
+template <int D, bool FP8, int WR>
+__global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
+  constexpr int NSTEP = D / 16, NDB = D / 32, ESZ = FP8 ? 1 : 2, WK = kWaves / WR, ROWS = 32 * WR;
+  constexpr int PITCH = D + 4;  // floats between rows of the waves' results in LDS
+  using Chunk = std::conditional_t<FP8, u32x2, u32x4>;
+  __shared__ __align__(16) float o_lds[WK > 1 ? kWaves * 32 * PITCH : 4];
+  __shared__ float ml_lds[kWaves][32][2];
+  __shared__ long long sums[kWaves];
+  __shared__ long long found_base;
+  __shared__ int found_seq;
+
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
+  const int group = p.n_q_heads / p.n_kv_heads;
+
+  // ---- this work-group's share: thread t sums the units of sequences [t per, (t + 1) per)
+  const int per = (p.n_seqs + kThreads - 1) / kThreads;
+  const int s_lo = min(tid * per, p.n_seqs), s_hi = min(s_lo + per, p.n_seqs);
+  auto units_of = [&](const Lens& n) { return n.count ? (long long)row_tiles<WR>(p, n) * key_units(n) * p.n_kv_heads : 0LL; };
+  long long mine = 0;
+  for (int s = s_lo; s < s_hi; ++s) mine += units_of(lens_of(p, s));
+  long long incl = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const long long y = __shfl(incl, lane - d < 0 ? lane : lane - d);
+    if (lane >= d) incl += y;
+  }
+  if (lane == 63) sums[wave] = incl;
+  __syncthreads();
+  long long total = 0, base = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w == wave) base = total;
+    total += sums[w];
+  }
+  base += incl - mine;
+  const int active = (int)min((long long)gridDim.x, total);
+  int share = blockIdx.x;
+  bool idle = share >= active;
+  if (gridDim.x % kQueues == 0) {
+    const int xcd = share % kQueues, first = xcd * active / kQueues;
+    share = first + share / kQueues;
+    idle = share >= (xcd + 1) * active / kQueues;
+  }
+  if (tid == 0) p.splits[blockIdx.x].n_pieces = 0;
+  if (idle) return;
+  const long long begin = share * total / active, end = (share + 1) * total / active;
+  if (base <= begin && begin < base + mine) {  // one thread
+    int s = s_lo;
+    for (;; ++s) {
+      const long long u = units_of(lens_of(p, s));
+      if (begin < base + u) break;
+      base += u;
+    }
+    found_seq = s;
+    found_base = base;
+  }
+  __syncthreads();
+  int s = __builtin_amdgcn_readfirstlane(found_seq);
+  long long seq_base = found_base, at = begin;
+  Lens n = lens_of(p, s);
+
+  while (at < end) {
+    // ---- the piece: units of one row tile
+    while (n.count == 0 || at >= seq_base + units_of(n)) {  // the share has another unit, so there is another sequence
+      seq_base += units_of(n);
+      n = lens_of(p, ++s);
+    }
+    const int n_key_units = key_units(n), n_tiles = row_tiles<WR>(p, n), kv_len = n.prefix + n.count;
+    const long long rel = at - seq_base;
+    const int tile_index = (int)(rel / n_key_units), unit = (int)(rel - (long long)tile_index * n_key_units);
+    const int kv_head = tile_index / n_tiles, tile = tile_index - kv_head * n_tiles;
+    const long long item_end = at - unit + n_key_units;
+    const long long piece_end = min(item_end, end);
+    const int key_begin = unit * kUnitKeys, key_end = min(kv_len, (unit + (int)(piece_end - at)) * kUnitKeys);
+    const int row0 = tile * ROWS, n_rows = min(ROWS, n.count * group - row0);
+    const bool whole = unit == 0 && piece_end == item_end;
+
+    // ---- rows
+    const int row = min(row0 + wr * 32 + c32, n.count * group - 1);
+    const int token = row / group, head = kv_head * group + row - token * group;
+    float c = p.scale_log2e * (FP8 ? p.k_scale[kv_head] : 1.0f);
+    const unsigned flip = c < 0 ? 0x80008000u : 0u;  // the running maximum is that of the scores: a negative factor goes into q
+    c = fabsf(c);
+    if (c < 1e-37f) c = 1e-37f;  // and 0 times the -infinity of a key that is not seen is no weight
+    bf16x8 qreg[NSTEP];
+    const unsigned short* qp = p.q + ((long long)(n.first + token) * p.n_q_heads + head) * D + 8 * half;
+#pragma unroll
+    for (int st = 0; st < NSTEP; ++st) qreg[st] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + 16 * st) ^ flip);
+
+    f32x16 o[NDB];
+    float m = kNeg, l = 0.f;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+
+    // ---- keys: sub-tiles wk, wk + WK, ... of the piece
+    const int* table = p.block_tables + (long long)s * p.max_blocks;
+    const int last_block = (kv_len - 1) / kBlock;
+    const long long head_bytes = 16 * D * ESZ;
+    const int pr = perm32(c32);
+    const int k_off = (half * 16 + (pr & 15)) * 8 * ESZ, v_off = (half * D + pr) * 8 * ESZ;
+    Chunk k[NSTEP], v[NSTEP];
+    auto block_at = [&](int key, int b) { return (long long)table[min(key / kBlock + b, last_block)]; };
+    auto load_k = [&](long long b0, long long b1) {
+      const unsigned char* g = p.k_pool + (((pr >> 4) ? b1 : b0) * p.n_kv_heads + kv_head) * head_bytes + k_off;
+#pragma unroll
+      for (int st = 0; st < NSTEP; ++st) k[st] = *reinterpret_cast<const Chunk*>(g + st * 256 * ESZ);
+    };
+    auto load_v = [&](long long b0, long long b1) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const unsigned char* g = p.v_pool + ((t ? b1 : b0) * p.n_kv_heads + kv_head) * head_bytes + v_off;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) v[t * NDB + db] = *reinterpret_cast<const Chunk*>(g + db * 256 * ESZ);
+      }
+    };
+    auto operand = [&](Chunk x) {
+      if constexpr (FP8) return fp8x8_to_bf16x8(x);
+      else return x;
+    };
+    int key = key_begin + 32 * wk;
+    if (key < key_end) {
+      const long long b0 = block_at(key, 0), b1 = block_at(key, 1);
+      load_k(b0, b1);
+      load_v(b0, b1);
+    }
+    for (; key < key_end; key += 32 * WK) {
+      const int next = key + 32 * WK;
+      long long b0 = 0, b1 = 0;
+      if (next < key_end) b0 = block_at(next, 0), b1 = block_at(next, 1);
+      f32x16 sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+      for (int st = 0; st < NSTEP; ++st)
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(operand(k[st])), qreg[st], sc, 0, 0, 0);
+      if (next < key_end) load_k(b0, b1);
+      const bool tail = key + 32 > n.prefix;
+      unsigned seen = ~0u;
+      if (tail) {
+        seen = visible_bits(p, n, token, key);
+        const unsigned own = seen >> (8 * half);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = own >> (16 * (i >> 3) + (i & 7)) & 1 ? sc[i] : -__builtin_inff();
+      }
+      float mx = sc[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+      mx = pair_max(mx);
+      // m only has to bound the scores loosely: numerators of up to 2^kLazyLog2 are as exact in bf16 as those below 1
+      if (__builtin_amdgcn_ballot_w64((mx - m) * c > kLazyLog2) != 0) {
+        const float m_new = fmaxf(m, mx);
+        const float alpha = __builtin_amdgcn_exp2f((m - m_new) * c);
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+        m = m_new;
+      }
+      u32x4 pp[2];
+      l += softmax_exp_part(sc, c, m, pp);
+      u32x4 vop[NSTEP];
+#pragma unroll
+      for (int x = 0; x < NSTEP; ++x) vop[x] = operand(v[x]);
+      bool odd = false;
+      if (tail) {
+        if (key + 32 > kv_len) {
+#pragma unroll
+          for (int x = 0; x < NSTEP; ++x) vop[x] = zero_tail(vop[x], key + 16 * (x / NDB) + 8 * half, kv_len);
+        }
+#pragma unroll
+        for (int x = 0; x < NSTEP; ++x) odd |= not_finite(vop[x]);
+      }
+      if (tail && __builtin_amdgcn_ballot_w64(odd) != 0) {
+        // An infinite or NaN value that some rows do not see: 0 times it would be NaN, so their sums leave the key out.
+        for (int b = 0; b < 32; ++b) {
+          const int x = (b >> 4) * 4 + ((b & 7) >> 1);
+          unsigned word = 0;
+#pragma unroll
+          for (int y = 0; y < 8; ++y) word = x == y ? pp[y >> 2][y & 3] : word;
+          word = __shfl(word, c32 + 32 * (b >> 3 & 1));
+          const float weight = __uint_as_float(b & 1 ? word & 0xffff0000u : word << 16);
+          const int pos = key + b;
+          if (pos >= kv_len) break;
+          const unsigned char* g = p.v_pool + (block_at(pos, 0) * p.n_kv_heads + kv_head) * head_bytes + (pos % kBlock / 8 * D * 8 + pos % 8) * ESZ;
+#pragma unroll
+          for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int d = 32 * db + 16 * (i >> 3) + 8 * half + (i & 7);
+              float value;
+              if constexpr (FP8) value = __builtin_amdgcn_cvt_f32_fp8((int)g[d * 8], 0);
+              else value = __uint_as_float((unsigned)reinterpret_cast<const unsigned short*>(g)[d * 8] << 16);
+              o[db][i] = seen >> b & 1 ? __builtin_fmaf(weight, value, o[db][i]) : o[db][i];
+              asm volatile("" : "+v"(o[db][i]) : : "memory");  // one value after the other: no registers for a path that is hardly ever taken
+            }
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int db = 0; db < NDB; ++db)
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vop[t * NDB + db]), as_bf16x8(pp[t]), o[db], 0, 0, 0);
+      }
+      if (next < key_end) load_v(b0, b1);
+    }
+    l = pair_sum(l);
+
+    // ---- results: final rows, or a slot of the partial results
+    const int slot = 2 * share + (unit == 0 ? 1 : 0);
+    float* part = p.partials + (long long)slot * kSlotFloats<D, WR>;
+    const float v_factor = FP8 ? p.v_scale[kv_head] : 1.0f;
+    auto store_final = [&](int r, int d, float (&x)[8], float sum) {  // 8 dims of row r of the tile
+      const int tok = (row0 + r) / group, h = kv_head * group + (row0 + r) - tok * group;
+      float f = v_factor / sum;
+      u32x4 w;
+      if (sum == 0.f && sees_nothing(p, n, tok)) {
+        w = u32x4{0, 0, 0, 0};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = pack_bf16(x[2 * e] * f, x[2 * e + 1] * f);
+      }
+      *reinterpret_cast<u32x4*>(p.out + ((long long)(n.first + tok) * p.n_q_heads + h) * D + d) = w;
+    };
+    auto store_partial = [&](int r, int d, const float (&x)[8]) {
+      float* to = part + r * D + d;
+      *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
+      *reinterpret_cast<f32x4*>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    };
+    if constexpr (WK == 1) {
+      const int r = wr * 32 + c32;
+      if (r < n_rows) {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = o[db][8 * h + e];
+            const int d = 32 * db + 16 * h + 8 * half;
+            if (whole) store_final(r, d, x, l);
+            else store_partial(r, d, x);
+          }
+        if (!whole && half == 0) {
+          part[ROWS * D + 2 * r] = m * c;
+          part[ROWS * D + 2 * r + 1] = l;
+        }
+      }
+    } else {
+      float* mine_o = o_lds + (wave * 32 + c32) * PITCH;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+          *reinterpret_cast<f32x4*>(mine_o + 32 * db + 16 * (h >> 1) + 8 * half + 4 * (h & 1)) =
+              f32x4{o[db][4 * h], o[db][4 * h + 1], o[db][4 * h + 2], o[db][4 * h + 3]};
+      if (half == 0) {
+        ml_lds[wave][c32][0] = m * c;
+        ml_lds[wave][c32][1] = l;
+      }
+      __syncthreads();
+      for (int x = tid; x < n_rows * (D / 8); x += kThreads) {
+        const int r = x / (D / 8), d = x % (D / 8) * 8, w0 = r / 32 * WK, rr = r % 32;
+        float top = ml_lds[w0][rr][0], sum = 0.f;
+#pragma unroll
+        for (int w = 1; w < WK; ++w) top = fmaxf(top, ml_lds[w0 + w][rr][0]);
+        float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WK; ++w) {
+          const float f = __builtin_amdgcn_exp2f(ml_lds[w0 + w][rr][0] - top);
+          sum = __builtin_fmaf(f, ml_lds[w0 + w][rr][1], sum);
+          const float* from = o_lds + ((w0 + w) * 32 + rr) * PITCH + d;
+          const f32x4 a = *reinterpret_cast<const f32x4*>(from), b = *reinterpret_cast<const f32x4*>(from + 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            acc[e] = __builtin_fmaf(f, a[e], acc[e]);
+            acc[4 + e] = __builtin_fmaf(f, b[e], acc[4 + e]);
+          }
+        }
+        if (whole) {
+          store_final(r, d, acc, sum);
+        } else {
+          store_partial(r, d, acc);
+          if (d == 0) {
+            part[ROWS * D + 2 * r] = top;
+            part[ROWS * D + 2 * r + 1] = sum;
+          }
+        }
+      }
+      __syncthreads();
+    }
+    if (unit == 0 && !whole && tid == 0) {
+      int last = share + 1;
+      while ((last + 1) * total / active < item_end) ++last;
+      p.splits[blockIdx.x] = Split{last - share + 1, share, n_rows, row0, kv_head, n.first, n.prefix, n.count};
+    }
+    at = piece_end;
+  }
+}
+
+// Combines the pieces of the row tile that work-group blockIdx.x began and others went on with; a thread has 4 dims of a row.
+template <int D, bool FP8, int WR>
+__global__ __launch_bounds__(256) void merge_kernel(TreeParams p) {
+  constexpr int kRows = 1024 / D, ROWS = 32 * WR;
+  const Split sp = p.splits[blockIdx.x];
+  const int r = blockIdx.y * kRows + (int)threadIdx.x / (D / 4), d = (int)threadIdx.x % (D / 4) * 4;
+  if (r >= (sp.n_pieces ? sp.n_rows : 0)) return;
+  float top = kNeg, sum = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < sp.n_pieces; ++i) {
+    const float* part = p.partials + (long long)(2 * (sp.share + i) + (i == 0)) * kSlotFloats<D, WR>;
+    const float m = part[ROWS * D + 2 * r], l = part[ROWS * D + 2 * r + 1];
+    const f32x4 o = *reinterpret_cast<const f32x4*>(part + r * D + d);
+    const float m_new = fmaxf(top, m);
+    const float keep = __builtin_amdgcn_exp2f(top - m_new), add = __builtin_amdgcn_exp2f(m - m_new);
+    sum = sum * keep + l * add;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = acc[e] * keep + o[e] * add;
+    top = m_new;
+  }
+  const int group = p.n_q_heads / p.n_kv_heads, token = (sp.row0 + r) / group, head = sp.kv_head * group + (sp.row0 + r) - token * group;
+  const float f = (FP8 ? p.v_scale[sp.kv_head] : 1.0f) / sum;
+  u32x2 w = {pack_bf16(acc[0] * f, acc[1] * f), pack_bf16(acc[2] * f, acc[3] * f)};
+  if (sum == 0.f && sees_nothing(p, Lens{sp.prefix, sp.count, sp.first_token}, token)) w = u32x2{0, 0};
+  *reinterpret_cast<u32x2*>(p.out + ((long long)(sp.first_token + token) * p.n_q_heads + head) * D + d) = w;
+}
+
+// Wavefronts side by side: as many as it takes for a sequence's rows of a KV head, up to all.
+int waves_of_rows(const cronus_kv_cache* cache, int32_t max_rows) {
+  const long long rows = (long long)max_rows * (cache->num_q_heads / cache->num_kv_heads);
+  return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+}
+
+size_t split_bytes(int n_cus) { return ((size_t)n_cus * sizeof(Split) + 255) / 256 * 256; }
+
+template <int D, bool FP8, int WR>
+int launch(const TreeParams& p, int n_cus, hipStream_t stream) {
+  hipLaunchKernelGGL((attn_tree_kernel<D, FP8, WR>), dim3(n_cus), dim3(kThreads), 0, stream, p);
+  if (hipGetLastError() != hipSuccess) return CRONUS_ERR_HIP;
+  hipLaunchKernelGGL((merge_kernel<D, FP8, WR>), dim3(n_cus, 32 * WR * D / 1024), dim3(256), 0, stream, p);
+  return hipGetLastError() == hipSuccess ? CRONUS_OK : CRONUS_ERR_HIP;
+}
+template <int D, bool FP8>
+int launch_rows(const TreeParams& p, int waves, int n_cus, hipStream_t stream) {
+  switch (waves) {
+    case 1: return launch<D, FP8, 1>(p, n_cus, stream);
+    case 2: return launch<D, FP8, 2>(p, n_cus, stream);
+    case 4: return launch<D, FP8, 4>(p, n_cus, stream);
+    default: return launch<D, FP8, 8>(p, n_cus, stream);
+  }
+}
+
+}  // namespace
+
+size_t attn_tree_workspace(const cronus_kv_cache* cache, int32_t max_rows, int n_cus) {
+  const size_t slot = (size_t)32 * waves_of_rows(cache, max_rows) * (cache->head_dim + 2) * sizeof(float);
+  return split_bytes(n_cus) + (2 * slot * n_cus + 255) / 256 * 256;
+}
+
+int launch_attn_tree(const cronus_kv_cache* cache, const void* q, void* out, const int32_t* prefix_lens, const int32_t* cu_rows,
+                     const uint64_t* mask, int32_t mask_words, const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t n_seqs,
+                     int32_t max_rows, float sm_scale, void* workspace, int n_cus, void* stream) {
+  TreeParams p{};
+  p.q = static_cast<const unsigned short*>(q);
+  p.out = static_cast<unsigned short*>(out);
+  p.k_pool = static_cast<const unsigned char*>(cache->k_cache);
+  p.v_pool = static_cast<const unsigned char*>(cache->v_cache);
+  p.k_scale = cache->k_scale;
+  p.v_scale = cache->v_scale;
+  p.prefix_lens = prefix_lens;
+  p.cu_rows = cu_rows;
+  p.mask = reinterpret_cast<const unsigned long long*>(mask);
+  p.mask_words = mask_words;
+  p.block_tables = block_tables;
+  p.max_blocks = max_blocks_per_seq;
+  p.n_seqs = n_seqs;
+  p.max_rows = max_rows;
+  p.n_q_heads = cache->num_q_heads;
+  p.n_kv_heads = cache->num_kv_heads;
+  p.scale_log2e = sm_scale * 1.4426950408889634f;
+  p.splits = static_cast<Split*>(workspace);
+  p.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + split_bytes(n_cus));
+  const int waves = waves_of_rows(cache, max_rows);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool fp8 = cache->kv_dtype == CRONUS_KV_FP8_E4M3;
+  if (cache->head_dim == 128) return fp8 ? launch_rows<128, true>(p, waves, n_cus, s) : launch_rows<128, false>(p, waves, n_cus, s);
+  return fp8 ? launch_rows<64, true>(p, waves, n_cus, s) : launch_rows<64, false>(p, waves, n_cus, s);
+}
+
+}  // namespace cronus

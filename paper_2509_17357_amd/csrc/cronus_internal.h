@@ -325,6 +325,26 @@ int launch_kv_gather(const cronus_kv_cache* cache, void* k_dst, void* v_dst, con
                      const int32_t* start_pos, const int32_t* block_tables, int32_t max_blocks_per_seq,
                      int32_t n_seqs, int32_t n_tokens, void* stream);
 
+// api.cpp: CU count of the current device; 256 (MI355X) when sizes are queried without a device
+int device_cus();
+
+// build_tables.hip
+int launch_build_tables(const cronus_paged_tables* tables, const int32_t* kv_lens, const int32_t* new_lens, int32_t n_seqs,
+                        int32_t* cu_tokens, int32_t* start_pos, int32_t* cu_blocks, int64_t* slot_map, int32_t max_tokens,
+                        int32_t* report, void* stream);
+
+// attn_tree.hip
+constexpr long long kTreeMostKeys = 0x7fffff00LL;  // keys of a sequence: positions up to a sub-tile further stay in 32 bits
+size_t attn_tree_workspace(const cronus_kv_cache* cache, int32_t max_rows, int n_cus);
+int launch_attn_tree(const cronus_kv_cache* cache, const void* q, void* out, const int32_t* prefix_lens, const int32_t* cu_rows,
+                     const uint64_t* mask, int32_t mask_words, const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t n_seqs,
+                     int32_t max_rows, float sm_scale, void* workspace, int n_cus, void* stream);
+
+// kv_commit.hip; the caches agree in all but their pools
+int launch_kv_commit(const cronus_kv_cache* caches, int32_t n_caches, const int32_t* start_pos, const int32_t* cu_rows,
+                     const int32_t* paths, int32_t max_path, const int32_t* path_lens, const int32_t* block_tables,
+                     int32_t max_blocks_per_seq, int32_t n_seqs, int32_t* kv_lens_out, void* stream);
+
 // mfma_probe.hip (measurement aid)
 int launch_mfma_probe(bool small_shape, int random_operands, int iters, int n_cus, float* sink, void* stream, double* flops);
 int mfma_probe_sink_floats(int n_cus);

@@ -8,6 +8,7 @@ The hot path of one iteration (Cronus section 4.2 and 4.4) is, in order:
                       1 and 2 in one launch (cronus_kv_append_pair)
   3. attention      - cronus_attn_mixed over chunks and decodes; a step is one call for all three
                       (cronus_iteration)
+DraftLoop holds the state of a loop whose lengths live on the device (drafted tokens verified as a tree).
 The contexts of the decode requests were cached by earlier iterations; here they are
 placed by setup_decode_context(), which is set-up, not part of the iteration.
 """
@@ -182,3 +183,63 @@ class DeviceIteration:
         self.ensure_workspace()
         B.cronus_iteration(self.cache, *self._rows(), self.q, self.out, b.prefix_lens, b.chunk_lens, self.block_tables,
                            b.max_blocks, self.sm_scale, self.workspace, self.workspace_bytes, self._stream())
+
+
+class DraftLoop:
+    """Device state of a loop that drafts tokens and keeps the accepted ones: every layer's cache, the tables, the free list and
+    the lengths, none of which the host reads.  An iteration is
+      1. begin    - cronus_build_tables: blocks for the new rows of every sequence (-1: the sequence has ended)
+      2. per layer  append (cronus_kv_append) and attend (cronus_attn_tree)
+      3. commit   - cronus_kv_commit: the accepted path's rows stay, the lengths grow by them
+    all on the current stream.  Nothing is allocated after construction, so an iteration can be captured into a graph (not across a
+    change of the tensors that are passed in).  `report` says whether the blocks sufficed; where they did not, the iteration leaves
+    everything as it was."""
+
+    def __init__(self, shape, n_layers: int, n_seqs: int, num_blocks: int, max_blocks: int, max_rows: int, max_path: int,
+                 device="cuda:0", scales=None, pool_fill=0):
+        self.shape, self.n_seqs, self.max_blocks, self.max_rows, self.max_path = shape, n_seqs, max_blocks, max_rows, max_path
+        self.num_blocks, self.max_tokens = num_blocks, n_seqs * max_rows
+        self.device = torch.device(device)
+        fp8 = shape.kv_dtype == "fp8"
+        size = num_blocks * shape.n_kv_heads * 16 * shape.head_dim
+        pool = lambda: [torch.full((size,), pool_fill, dtype=torch.uint8 if fp8 else torch.int16, device=self.device) for _ in range(n_layers)]
+        self.k_pools, self.v_pools = pool(), pool()
+        self.scales = [None if s is None else torch.as_tensor(s, dtype=torch.float32, device=self.device) for s in scales or (None, None)]
+        caches = [B.make_cache(k, v, num_blocks, shape.n_q_heads, shape.n_kv_heads, shape.head_dim,
+                               B.CRONUS_KV_FP8_E4M3 if fp8 else B.CRONUS_KV_BF16, *self.scales) for k, v in zip(self.k_pools, self.v_pools)]
+        self.caches = B.cache_array(caches)
+        i32 = lambda *n, fill=0: torch.full(n, fill, dtype=torch.int32, device=self.device)
+        self.block_tables, self.held, self.kv_lens = i32(n_seqs, max_blocks, fill=-1), i32(n_seqs), i32(n_seqs)
+        self.free_blocks, self.free_count = torch.arange(num_blocks, dtype=torch.int32, device=self.device), i32(1, fill=num_blocks)
+        self.cu_rows, self.start_pos, self.cu_blocks, self.report = i32(n_seqs + 1), i32(n_seqs), i32(n_seqs + 1), i32(4)
+        self.slot_map = torch.full((self.max_tokens,), -1, dtype=torch.int64, device=self.device)
+        self.sm_scale = 1.0 / float(np.sqrt(shape.head_dim))
+        self.workspace_bytes = B.cronus_attn_tree_workspace_bytes(self.caches[0], max_rows)
+        if self.workspace_bytes == 0:
+            raise RuntimeError("cronus_attn_tree_workspace_bytes rejected the shape")
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+
+    def _stream(self):
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def begin(self, new_lens):
+        """new_lens: device int32 [n_seqs]."""
+        return B.cronus_build_tables((self.block_tables, self.max_blocks, self.held, self.held, self.free_blocks, self.num_blocks,
+                                      self.free_count, self.free_count), self.kv_lens, new_lens, self.n_seqs, self.cu_rows,
+                                     self.start_pos, self.cu_blocks, self.slot_map, self.max_tokens, self.report, self._stream())
+
+    def append(self, layer: int, k, v):
+        """k, v: the new rows of all sequences, back to back (bf16 [rows][Hkv][D]; rows behind the last sequence's are not read)."""
+        return B.cronus_kv_append(self.caches[layer], k, v, self.cu_rows, self.start_pos, self.block_tables, self.max_blocks,
+                                  self.n_seqs, k.shape[0], self._stream())
+
+    def attend(self, layer: int, q, out, mask=None):
+        """mask: int64 [rows][words], None for a chain."""
+        return B.cronus_attn_tree(self.caches[layer], q, out, self.start_pos, self.cu_rows, mask, 0 if mask is None else mask.shape[1],
+                                  self.block_tables, self.max_blocks, self.n_seqs, self.max_rows, self.sm_scale, self.workspace,
+                                  self.workspace_bytes, self._stream())
+
+    def commit(self, paths, path_lens):
+        """paths: device int32 [n_seqs][max_path]; path_lens: device int32 [n_seqs]."""
+        return B.cronus_kv_commit(self.caches, self.start_pos, self.cu_rows, paths, self.max_path, path_lens, self.block_tables,
+                                  self.max_blocks, self.n_seqs, self.kv_lens, self._stream())

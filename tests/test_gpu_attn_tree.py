@@ -1,0 +1,299 @@
+"""cronus_attn_tree against attention in 64 bits, with the error that its arithmetic allows (draft_util.attention)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cronus_oracle as orc
+from paper_2509_17357_amd import binding as B
+from paper_2509_17357_amd import workloads as W
+from paper_2509_17357_amd.runtime import bf16_tensor_from_bits, bits_from_bf16_tensor
+
+import draft_util as D
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+SHAPES = {"small": (8, 2, 64), "usual": (32, 8, 128), "g7": (28, 4, 128), "big": (64, 8, 128), "mha": (3, 3, 64), "g1": (2, 2, 128),
+          "mqa": (40, 1, 64)}
+
+
+class Batch:
+    """Pools full of NaN but for the sequences' own K/V; host copies of everything."""
+
+    def __init__(self, shape, dt, prefix, count, seed, masks="tree", words=None, first_row=0, q_scale=2.0, scales=None, spare=3):
+        self.hq, self.hkv, self.d = SHAPES[shape] if isinstance(shape, str) else shape
+        rng = self.rng = np.random.default_rng(seed)
+        self.fp8 = dt == "fp8"
+        self.prefix, self.count = np.array(prefix, np.int32), np.array(count, np.int32)
+        self.cu = (first_row + np.concatenate([[0], np.cumsum(np.maximum(self.count, 0))])).astype(np.int32)
+        self.n, self.rows = len(prefix), int(self.cu[-1])
+        self.max_rows = max(1, int(self.count.max()))
+        kv = np.maximum(self.prefix.astype(np.int64), 0) + np.maximum(self.count, 0)
+        blocks = -(-kv // 16)
+        self.width = max(1, int(blocks.max()))
+        self.num_blocks = int(blocks.sum()) + spare
+        ids = rng.permutation(self.num_blocks)
+        self.table = np.full((self.n, self.width), -1, np.int32)
+        self.k_pool = np.full(self.num_blocks * self.hkv * 16 * self.d, 0x7F if self.fp8 else 0x7FC1, np.uint8 if self.fp8 else np.uint16)
+        self.v_pool = self.k_pool.copy()
+        self.scales = scales if scales is not None else ((rng.uniform(0.005, 0.02, self.hkv).astype(np.float32), rng.uniform(0.005, 0.02, self.hkv).astype(np.float32))
+                                                         if self.fp8 else (None, None))
+        self.kv_bits, at = [], 0
+        for s in range(self.n):
+            self.table[s, :blocks[s]] = ids[at:at + blocks[s]]
+            at += blocks[s]
+            draw = lambda: (rng.integers(0, 256, (kv[s], self.hkv, self.d)).astype(np.uint8) & 0xF7 if self.fp8  # noqa: E731  (no NaN codes)
+                            else W.normal_bf16(rng, (kv[s], self.hkv, self.d), 1.0))
+            self.kv_bits.append([draw(), draw()])
+        self.q_bits = W.normal_bf16(rng, (self.rows, self.hq, self.d), q_scale)
+        self.words = words or (self.max_rows + 63) // 64
+        self.seen, self.mask = [], None
+        if masks is not None:
+            self.mask = rng.integers(-2 ** 63, 2 ** 63 - 1, (self.rows, self.words))  # bits that no row owns are random
+            for s in range(self.n):
+                m = max(int(self.count[s]), 0)
+                rows, packed = D.random_tree_mask(rng, m, self.words, None if masks == "tree" else masks)
+                own = D.pack_mask(np.ones((1, m), dtype=bool), self.words)[0]
+                at = slice(self.cu[s], self.cu[s + 1])
+                self.mask[at] = packed | (self.mask[at] & ~own)
+                self.seen.append(rows)
+
+    def load(self):
+        for s, (k, v) in enumerate(self.kv_bits):
+            if len(k):
+                D.write_rows(self.k_pool, self.v_pool, self.hkv, self.d, self.table[s], np.arange(len(k)), k, v)
+        dev = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+        view = lambda a: dev(a if self.fp8 else a.view(np.int16))  # noqa: E731
+        self.t = {"k": view(self.k_pool), "v": view(self.v_pool), "table": dev(self.table), "prefix": dev(self.prefix), "cu": dev(self.cu),
+                  "mask": None if self.mask is None else dev(self.mask), "q": bf16_tensor_from_bits(self.q_bits, DEV),
+                  "ks": None if self.scales[0] is None else dev(self.scales[0]), "vs": None if self.scales[1] is None else dev(self.scales[1])}
+        self.t["out"] = torch.full((self.rows, self.hq, self.d), 7.25, dtype=torch.bfloat16, device=DEV)
+        self.cache = B.make_cache(self.t["k"], self.t["v"], self.num_blocks, self.hq, self.hkv, self.d,
+                                  B.CRONUS_KV_FP8_E4M3 if self.fp8 else B.CRONUS_KV_BF16, self.t["ks"], self.t["vs"])
+        self.ws_bytes = B.cronus_attn_tree_workspace_bytes(self.cache, self.max_rows)
+        self.t["ws"] = torch.full((self.ws_bytes,), 0xFF, dtype=torch.uint8, device=DEV)  # NaN
+        self.sm_scale = 1.0 / float(np.sqrt(self.d))
+        return self
+
+    def call(self, **kw):
+        a = {**self.t, **kw}
+        B.cronus_attn_tree(self.cache, a["q"], a["out"], a["prefix"], a["cu"], a["mask"], self.words, a["table"], self.width, self.n,
+                           kw.get("max_rows", self.max_rows), self.sm_scale, a["ws"], self.ws_bytes, torch.cuda.current_stream().cuda_stream)
+
+    def run(self):
+        self.load()
+        self.call()
+        torch.cuda.synchronize()
+        return self.got()
+
+    def got(self):
+        return orc.bf16_bits_to_f64(bits_from_bf16_tensor(self.t["out"]))
+
+    def expected(self, s):
+        m, at = int(self.count[s]), slice(self.cu[s], self.cu[s + 1])
+        k, v = (D.values(bits, scale) for bits, scale in zip(self.kv_bits[s], self.scales))
+        seen = D.seen_of(int(self.prefix[s]), m, None if self.mask is None else self.seen[s])
+        return D.attention(orc.bf16_bits_to_f64(self.q_bits[at]), k, v, seen, self.sm_scale)
+
+    def check(self, got=None, seqs=None):
+        got = self.run() if got is None else got
+        for s in range(self.n) if seqs is None else seqs:
+            if self.count[s] <= 0:
+                continue
+            x = got[self.cu[s]:self.cu[s + 1]]
+            ref, bound = self.expected(s)
+            assert np.array_equal(np.isnan(ref), np.isnan(x)), (s, "NaN")
+            fine = np.isfinite(ref)
+            assert np.array_equal(x[~fine & ~np.isnan(ref)], ref[~fine & ~np.isnan(ref)]), (s, "infinities")
+            off = np.abs(x[fine] - ref[fine]) - bound[fine]
+            assert (off <= 0).all(), (s, int(self.prefix[s]), int(self.count[s]), float(off.max()), int((off > 0).sum()), off.size)
+        return got
+
+
+EDGES = [0, 1, 15, 16, 17, 31, 32, 33, 47, 63, 64, 65, 127, 250, 255, 256, 257, 300, 511, 513]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp8"])
+@pytest.mark.parametrize("shape", list(SHAPES))
+@pytest.mark.parametrize("most", [1, 4, 9, 31, 70])
+def test_trees_behind_prefixes_of_every_alignment(shape, dt, most):
+    rng = np.random.default_rng(most)
+    Batch(shape, dt, EDGES, rng.integers(1, most, len(EDGES), endpoint=True), seed=100 + most, words=(most + 63) // 64).check()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp8"])
+@pytest.mark.parametrize("shape,most", [("small", 1), ("usual", 1), ("g7", 5), ("big", 16), ("usual", 130), ("mha", 64)])
+def test_chains(shape, dt, most):
+    rng = np.random.default_rng(most)
+    Batch(shape, dt, EDGES, rng.integers(1, most, len(EDGES), endpoint=True), seed=200 + most, masks=None).check()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp8"])
+@pytest.mark.parametrize("density", [0.0, 0.02, 0.5, 1.0])
+def test_any_mask_and_rows_that_see_nothing(dt, density):
+    b = Batch("usual", dt, [0, 0, 0, 5, 40, 0, 1000], [1, 30, 64, 33, 20, 130, 100], seed=300, masks=density, words=3)
+    got = b.check()
+    if density == 0.0:
+        assert (got[b.cu[0]:b.cu[3]] == 0).all() and (got[b.cu[3]:b.cu[4]] != 0).any()
+
+
+@pytest.mark.parametrize("shape,dt,prefix,count", [
+    ("usual", "bf16", [40000], [5]), ("small", "fp8", [70001], [1]), ("big", "fp8", [9000, 20, 17000], [64, 3, 33]),
+    ("g7", "bf16", [5000, 0, 12000, 1], [64, 64, 1, 20]), ("usual", "bf16", [3000] * 9, [13] * 9), ("mqa", "bf16", [6000, 100], [40, 2])])
+@pytest.mark.parametrize("masks", ["tree", None])
+def test_long_contexts_split_over_work_groups(shape, dt, prefix, count, masks):
+    Batch(shape, dt, prefix, count, seed=400, masks=masks).check()
+
+
+@pytest.mark.parametrize("n,count", [(600, 1), (1500, 3), (513, 8)])
+def test_many_sequences(n, count):
+    rng = np.random.default_rng(n)
+    c = rng.integers(0, count, n, endpoint=True)
+    Batch("small", "bf16", rng.integers(0, 120, n), np.maximum(c, 1 if count == 1 else 0), seed=n).check(seqs=None)
+
+
+def test_sequences_that_do_not_fit_are_passed_over():
+    b = Batch("small", "bf16", [40, 100, 20, 33, 64, 50], [5, 6, 0, 9, 3, 7], seed=500, first_row=4)
+    b.load()
+    want = b.check(got=(b.call(), torch.cuda.synchronize(), b.got())[2])
+    assert (want[:4] == 7.25).all()  # rows before the first sequence
+    wide = b.width * 16
+
+    def passed_over(seqs, **kw):
+        b.t["out"].fill_(7.25)
+        b.call(**kw)
+        torch.cuda.synchronize()
+        got = b.got()
+        assert (got[:4] == 7.25).all()
+        for s in seqs:
+            assert (got[b.cu[s]:b.cu[s + 1]] == 7.25).all(), s
+        b.check(got=got, seqs=[s for s in range(b.n) if s not in seqs])
+
+    for change in ({1: -1}, {1: wide - 5}, {3: wide}, {0: -2 ** 31}, {5: 2 ** 31 - 1}, {0: -7, 5: wide - 6}, {2: -1},
+                   {s: -1 for s in range(6)}):
+        prefix = b.prefix.copy()
+        for s, x in change.items():
+            prefix[s] = x
+        passed_over([s for s in change if b.count[s]], prefix=torch.from_numpy(prefix).to(DEV))
+    passed_over([3], max_rows=7)  # a sequence of more rows than max_rows
+    cu = b.cu.copy()
+    cu[4] = cu[3] - 1  # offsets that fall: sequence 3 has a negative number of rows, sequence 4 more than max_rows
+    passed_over([3, 4], cu=torch.from_numpy(cu).to(DEV))
+    assert np.isfinite(want).all()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp8"])
+@pytest.mark.parametrize("shape,count", [("small", 7), ("usual", 20), ("usual", 70)])
+def test_infinities_and_nan_of_hidden_tokens(shape, dt, count):
+    b = Batch(shape, dt, [37, 0, 300, 16], [count] * 4, seed=600)
+    bad = [0x7F] if dt == "fp8" else [0x7FC0, 0x7F80, 0xFF80]
+    for s in range(4):
+        for x, j in enumerate((1, count - 1, count // 2)):
+            for which in (0, 1) if s % 2 else (1,):
+                b.kv_bits[s][which][b.prefix[s] + j, x % b.hkv, (5 * x + s) % b.d] = bad[x % len(bad)]
+    got = b.check()
+    assert np.isfinite(got).any() and not np.isfinite(got).all()
+    # in a cached key they reach every row
+    b = Batch(shape, dt, [37, 90], [count] * 2, seed=601)
+    b.kv_bits[0][1][20, 0, 3] = bad[0]
+    b.kv_bits[1][0][89, 1, 0] = bad[0]
+    b.check()
+
+
+def test_scores_of_any_size():
+    for q_scale in (0.0, 1e-3, 60.0, 3e4):
+        Batch("usual", "bf16", [100, 1, 0, 700], [9, 20, 33, 2], seed=700, q_scale=q_scale).check()
+    # fp8 scales of any sign, and zero
+    k = np.array([0.01, -0.01, 0.0, 1.0, -0.02, 1e-30, 0.004, 0.01], np.float32)
+    v = np.array([-0.01, 0.01, 0.01, 0.0, 1.0, 0.01, 1e-30, 100.0], np.float32)
+    Batch("usual", "fp8", [100, 0, 700], [9, 33, 2], seed=701, scales=(k, v)).check()
+
+
+def test_same_bits_again_and_as_a_chain_near_the_mixed_attention():
+    b = Batch("usual", "bf16", [2000, 100, 900, 0], [20, 1, 33, 64], seed=800, masks=None)
+    b.check()
+    first = b.t["out"].clone()
+    for _ in range(3):
+        b.t["out"].zero_()
+        b.t["ws"].random_(0, 256)
+        b.call()
+        assert torch.equal(b.t["out"], first)
+    # the mask of a chain gives the bits of no mask
+    chain = np.concatenate([D.pack_mask(np.tril(np.ones((m, m), dtype=bool)), b.words) for m in b.count])
+    b.t["out"].zero_()
+    b.call(mask=torch.from_numpy(chain).to(DEV))
+    assert torch.equal(b.t["out"], first)
+    # both are within their bound of the same attention
+    need = B.cronus_attn_mixed_workspace_bytes(b.cache, b.prefix, b.count)
+    ws, out = torch.empty(need, dtype=torch.uint8, device=DEV), torch.zeros_like(first)
+    B.cronus_attn_mixed(b.cache, b.t["q"], out, b.prefix, b.count, b.t["table"], b.width, b.sm_scale, ws, need, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    mixed, got = orc.bf16_bits_to_f64(bits_from_bf16_tensor(out)), b.got()
+    for s in range(b.n):
+        _, bound = b.expected(s)
+        at = slice(b.cu[s], b.cu[s + 1])
+        assert (np.abs(mixed[at] - got[at]) <= 2 * bound).all()
+
+
+def test_unaligned_rows_and_another_stream():
+    b = Batch("g7", "bf16", [70, 33], [5, 12], seed=900)
+    b.check()
+    first = b.t["out"].clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for shift in (1, 3):
+        pad = lambda t: torch.zeros(t.numel() + 8, dtype=t.dtype, device=DEV)  # noqa: E731
+        q, out = pad(b.t["q"]), pad(b.t["out"])
+        q[shift:shift + b.t["q"].numel()] = b.t["q"].view(-1)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            b.call(q=q[shift:], out=out[shift:])
+        torch.cuda.current_stream().wait_stream(side)
+        n = first.numel()
+        assert torch.equal(out[shift:shift + n], first.view(-1)) and (out[:shift] == 0).all() and (out[shift + n:] == 0).all()
+
+
+def test_replays_follow_the_lengths():
+    b = Batch("usual", "bf16", [500, 40, 1200], [12, 33, 5], seed=1000)
+    b.load()
+    b.call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.call()
+    full = b.prefix.copy()
+    for k, cut in enumerate(([0, 0, 0], [500, 3, 700], [100, 40, 1200], [0, 0, 0], [3, 17, 33])):
+        prefix = full - np.array(cut, np.int32)
+        b.t["prefix"].copy_(torch.from_numpy(prefix))
+        b.t["out"].fill_(7.25)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = b.t["out"].clone()
+        b.t["out"].fill_(7.25)
+        b.call()
+        torch.cuda.synchronize()
+        assert torch.equal(replayed, b.t["out"]), k
+        # a shorter prefix: the drafted tokens are those behind it
+        b.prefix = prefix
+        kv = b.kv_bits
+        b.kv_bits = [[x[:prefix[s] + b.count[s]] for x in kv[s]] for s in range(b.n)]
+        b.check(got=b.got())
+        b.kv_bits, b.prefix = kv, full
+
+
+def test_blocks_beyond_4_gib():
+    hq, hkv, d = SHAPES["big"]
+    num_blocks = (5 << 30) // (hkv * 16 * d * 2)
+    b = Batch("big", "bf16", [200, 31], [9, 20], seed=1100)
+    b.load()
+    small_k, small_v, table = b.t["k"], b.t["v"], b.table
+    k, v = (torch.empty(num_blocks * hkv * 16 * d, dtype=torch.int16, device=DEV) for _ in range(2))
+    per = hkv * 16 * d
+    moved = np.where(table >= 0, num_blocks - 1 - table, -1).astype(np.int32)
+    for i in range(b.num_blocks):
+        for to, src in ((k, small_k), (v, small_v)):
+            to[(num_blocks - 1 - i) * per:(num_blocks - i) * per] = src[i * per:(i + 1) * per]
+    b.cache = B.make_cache(k, v, num_blocks, hq, hkv, d)
+    b.call(table=torch.from_numpy(moved).to(DEV))
+    torch.cuda.synchronize()
+    b.check(got=b.got())
