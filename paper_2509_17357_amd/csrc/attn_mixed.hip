@@ -344,8 +344,6 @@ constexpr int attn_lds_bytes() {
 constexpr int kLoopLdsBytes = 2 * 64 + 2 * 4 * kQueues;
 // and then the compact list, where the launch has one.
 
-typedef __attribute__((address_space(3))) unsigned char lds_byte;
-
 // Items of queue x that are handed out without a ticket: work-group b starts with item b / 8
 // of queue b mod 8 (the dispatcher deals work-groups to the XCDs in turn), so the first
 // items of a launch need no atomic, and a launch with no more items than work-groups needs
@@ -478,12 +476,6 @@ __device__ __forceinline__ WorkItem unpack_record(int rec) {
 }
 
 // ------------------------------------------------- wide (chunk) tile: DMA-fed pipeline
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-  static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
-  asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
-}
-
 // Copy 1 KiB, global -> LDS, by one wave (lane i moves bytes [16 i, 16 i + 16)): g and dst
 // are the wave's bases (no lane term).  Four 4-byte-per-lane instructions measured the same.
 // lane16 = 16 x lane is opaque here, so that the instruction takes the base from scalar and a
@@ -492,32 +484,6 @@ __device__ __forceinline__ void dma_1k(const unsigned char* g, lds_byte* dst, un
   asm volatile("" : "+v"(lane16));
   typedef const __attribute__((address_space(1))) unsigned char global_byte;
   __builtin_amdgcn_global_load_lds((global_byte*)g + lane16, dst, 16, 0, 0);
-}
-
-// LDS reads of data that arrived by global_load_lds are written as asm, so that the
-// waits on those loads are the explicit vmcnt waits of the pipelines and nothing coarser
-// (the compiler would wait for every DMA in flight before any LDS read).  The reads and
-// the wait for them form ONE asm statement: its outputs are valid when it ends, so no
-// register copy the compiler may insert afterwards can see a value that has not arrived.
-template <int O0, int O1, int O2, int O3>
-__device__ __forceinline__ void lds_read4(u32x4& x0, u32x4& x1, u32x4& x2, u32x4& x3, unsigned addr) {
-  asm volatile(
-      "ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%6\n\t"
-      "ds_read_b128 %2, %4 offset:%7\n\tds_read_b128 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
-      : "=&v"(x0), "=&v"(x1), "=&v"(x2), "=&v"(x3)
-      : "v"(addr), "i"(O0), "i"(O1), "i"(O2), "i"(O3)
-      : "memory");
-}
-template <int O0, int O1, int O2, int O3, int O4, int O5, int O6, int O7>
-__device__ __forceinline__ void lds_read8(u32x4 (&x)[8], unsigned addr) {
-  asm volatile(
-      "ds_read_b128 %0, %8 offset:%9\n\tds_read_b128 %1, %8 offset:%10\n\t"
-      "ds_read_b128 %2, %8 offset:%11\n\tds_read_b128 %3, %8 offset:%12\n\t"
-      "ds_read_b128 %4, %8 offset:%13\n\tds_read_b128 %5, %8 offset:%14\n\t"
-      "ds_read_b128 %6, %8 offset:%15\n\tds_read_b128 %7, %8 offset:%16\n\ts_waitcnt lgkmcnt(0)"
-      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
-      : "v"(addr), "i"(O0), "i"(O1), "i"(O2), "i"(O3), "i"(O4), "i"(O5), "i"(O6), "i"(O7)
-      : "memory");
 }
 
 // Split form for the steady-state loop: a read is issued (`lds_issue1`), independent work
@@ -546,14 +512,6 @@ template <int N>
 __device__ __forceinline__ void lds_land1(u32x4& x) {
   asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(x) : "i"(N) : "memory");
 }
-// Read the NOPS 1-KiB operand planes of this lane (plane n at addr + 1024 n).
-template <int NOPS>
-__device__ __forceinline__ void lds_read_planes(u32x4 (&x)[NOPS], unsigned addr) {
-  static_assert(NOPS == 4 || NOPS == 8, "D = 64 or 128");
-  if constexpr (NOPS == 8) lds_read8<0, 1024, 2048, 3072, 4096, 5120, 6144, 7168>(x, addr);
-  else lds_read4<0, 1024, 2048, 3072>(x[0], x[1], x[2], x[3], addr);
-}
-
 // Row r of a tile = (token r / g, head r % g), r < 256 and g = heads per item <= 32:
 // the quotient as (r * row_magic(g)) >> 16.  With M = 65536 / g + d, 0 < d <= 2, the product
 // exceeds r * 65536 / g by at most 2 * 255 < 65536 / 32, so the floor is that of r / g.
@@ -1318,28 +1276,6 @@ __device__ __forceinline__ void place_rows_read(const AttnParams& p, const NewRo
 }
 
 // --------------------------------------------------------- narrow (decode-like) item
-// Operand chunks of 8 bytes picked out of a block image in LDS (fp8 codes).
-template <int O0, int O1, int O2, int O3, int O4, int O5, int O6, int O7>
-__device__ __forceinline__ void lds_read8_b64(u32x2 (&x)[8], unsigned addr) {
-  asm volatile(
-      "ds_read_b64 %0, %8 offset:%9\n\tds_read_b64 %1, %8 offset:%10\n\t"
-      "ds_read_b64 %2, %8 offset:%11\n\tds_read_b64 %3, %8 offset:%12\n\t"
-      "ds_read_b64 %4, %8 offset:%13\n\tds_read_b64 %5, %8 offset:%14\n\t"
-      "ds_read_b64 %6, %8 offset:%15\n\tds_read_b64 %7, %8 offset:%16\n\ts_waitcnt lgkmcnt(0)"
-      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
-      : "v"(addr), "i"(O0), "i"(O1), "i"(O2), "i"(O3), "i"(O4), "i"(O5), "i"(O6), "i"(O7)
-      : "memory");
-}
-template <int O0, int O1, int O2, int O3>
-__device__ __forceinline__ void lds_read4_b64(u32x2 (&x)[4], unsigned addr) {
-  asm volatile(
-      "ds_read_b64 %0, %4 offset:%5\n\tds_read_b64 %1, %4 offset:%6\n\t"
-      "ds_read_b64 %2, %4 offset:%7\n\tds_read_b64 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
-      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-      : "v"(addr), "i"(O0), "i"(O1), "i"(O2), "i"(O3)
-      : "memory");
-}
-
 template <int D, bool FP8, bool LIST, bool PLACES>
 __device__ __forceinline__ void run_narrow(const AttnParams& p, const WorkItem& it, const NewRows& rows, unsigned char* smem) {
   constexpr int NSTEP = D / 16, NDB = D / 32;

@@ -10,8 +10,12 @@
 //
 // Eight wavefronts: WR of them side by side hold 32 rows each (a row is a drafted token and a query head of the KV head), and
 // 8 / WR such groups take every (8 / WR)-th 32-key sub-tile.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: a row is a
-// column, its lanes are l and l + 32, P stays in registers, and the operands are the cache's own 16-byte chunks (8 bytes, fp8), loaded
-// straight into registers.
+// column, its lanes are l and l + 32, and P stays in registers.  K/V reach the operands in one of two ways (STAGED):
+//   streamed - few rows, bound by memory: every wave moves its own sub-tiles to LDS of its own, by DMA, so that loads in flight
+//              take no registers, and no wave waits for another;
+//   staged   - many rows, bound by products: the work-group moves tiles of kUnitKeys keys through registers (fp8 codes are
+//              converted there, once) to one of two LDS buffers, and all waves read their operands there, where each would
+//              fetch the same K/V otherwise.
 #include <hip/hip_runtime.h>
 
 #include "cronus_internal.h"
@@ -110,25 +114,33 @@ __device__ __forceinline__ bool not_finite(u32x4 v) {
   return found;
 }
 
-template <int D, bool FP8, int WR>
-__global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
-  constexpr int NSTEP = D / 16, NDB = D / 32, ESZ = FP8 ? 1 : 2, WK = kWaves / WR, ROWS = 32 * WR;
-  constexpr int PITCH = D + 4;  // floats between rows of the waves' results in LDS
-  using Chunk = std::conditional_t<FP8, u32x2, u32x4>;
-  __shared__ __align__(16) float o_lds[WK > 1 ? kWaves * 32 * PITCH : 4];
-  __shared__ float ml_lds[kWaves][32][2];
-  __shared__ long long sums[kWaves];
-  __shared__ long long found_base;
-  __shared__ int found_seq;
+// The chunk with 0 in the place of infinities and NaN.
+__device__ __forceinline__ u32x4 finite_only(u32x4 v) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if ((v[w] & 0x7f80u) == 0x7f80u) v[w] &= 0xffff0000u;
+    if ((v[w] & 0x7f800000u) == 0x7f800000u) v[w] &= 0x0000ffffu;
+  }
+  return v;
+}
 
-  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
-  const int group = p.n_q_heads / p.n_kv_heads;
+// A work-group's share of the batch, and the sequence that it begins in.
+struct Share {
+  long long begin, end, total, seq_base;  // units; seq_base: those before sequence seq
+  int index, active, seq;
+  bool idle;
+};
+struct ShareLds {
+  long long sums[kWaves], base;
+  int seq;
+};
 
-  // ---- this work-group's share: thread t sums the units of sequences [t per, (t + 1) per)
+// Thread t sums the units of sequences [t per, (t + 1) per).
+template <class Units>
+__device__ __forceinline__ Share find_share(const TreeParams& p, ShareLds& lds, const Units& units_of) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (p.n_seqs + kThreads - 1) / kThreads;
   const int s_lo = min(tid * per, p.n_seqs), s_hi = min(s_lo + per, p.n_seqs);
-  auto units_of = [&](const Lens& n) { return n.count ? (long long)row_tiles<WR>(p, n) * key_units(n) * p.n_kv_heads : 0LL; };
   long long mine = 0;
   for (int s = s_lo; s < s_hi; ++s) mine += units_of(lens_of(p, s));
   long long incl = mine;
@@ -137,41 +149,68 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
     const long long y = __shfl(incl, lane - d < 0 ? lane : lane - d);
     if (lane >= d) incl += y;
   }
-  if (lane == 63) sums[wave] = incl;
+  if (lane == 63) lds.sums[wave] = incl;
   __syncthreads();
-  long long total = 0, base = 0;
+  Share r{};
+  long long base = 0;
   for (int w = 0; w < kWaves; ++w) {
-    if (w == wave) base = total;
-    total += sums[w];
+    if (w == wave) base = r.total;
+    r.total += lds.sums[w];
   }
   base += incl - mine;
-  const int active = (int)min((long long)gridDim.x, total);
-  int share = blockIdx.x;
-  bool idle = share >= active;
+  r.active = (int)min((long long)gridDim.x, r.total);
+  r.index = blockIdx.x;
+  r.idle = r.index >= r.active;
   if (gridDim.x % kQueues == 0) {
-    const int xcd = share % kQueues, first = xcd * active / kQueues;
-    share = first + share / kQueues;
-    idle = share >= (xcd + 1) * active / kQueues;
+    const int xcd = r.index % kQueues, first = xcd * r.active / kQueues;
+    r.index = first + r.index / kQueues;
+    r.idle = r.index >= (xcd + 1) * r.active / kQueues;
   }
-  if (tid == 0) p.splits[blockIdx.x].n_pieces = 0;
-  if (idle) return;
-  const long long begin = share * total / active, end = (share + 1) * total / active;
-  if (base <= begin && begin < base + mine) {  // one thread
+  if (r.idle) return r;
+  r.begin = r.index * r.total / r.active;
+  r.end = (r.index + 1) * r.total / r.active;
+  if (base <= r.begin && r.begin < base + mine) {  // one thread
     int s = s_lo;
     for (;; ++s) {
       const long long u = units_of(lens_of(p, s));
-      if (begin < base + u) break;
+      if (r.begin < base + u) break;
       base += u;
     }
-    found_seq = s;
-    found_base = base;
+    lds.seq = s;
+    lds.base = base;
   }
   __syncthreads();
-  int s = __builtin_amdgcn_readfirstlane(found_seq);
-  long long seq_base = found_base, at = begin;
+  r.seq = __builtin_amdgcn_readfirstlane(lds.seq);
+  r.seq_base = lds.base;
+  return r;
+}
+
+template <int D, bool FP8, int WR, bool STAGED>
+__global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
+  constexpr int NSTEP = D / 16, NDB = D / 32, ESZ = FP8 ? 1 : 2, WK = kWaves / WR, ROWS = 32 * WR;
+  constexpr int BLKB = 16 * D * ESZ;            // bytes of one (block, head) of the cache
+  constexpr int SWZ = D / 4 - 1;                // results in LDS: group x of 4 dims of row r lies at x ^ (r & SWZ)
+  constexpr int RESULT = 32 * D * 4;            // bytes of a wave's result
+  constexpr int WAVE_LDS = 2 * NSTEP * 1024 + (FP8 ? 512 : 0);  // streamed: a wave's K and V planes, or two sets of block images (fp8)
+  constexpr int TILE = kUnitKeys * D * 2 * 2;   // staged: bytes of K and V of a tile
+  static_assert(WAVE_LDS >= RESULT, "a wave's result takes the place of its planes");
+  constexpr int LDS = STAGED ? (WK > 1 && kWaves * RESULT > 2 * TILE ? kWaves * RESULT : 2 * TILE) : kWaves * WAVE_LDS;
+  __shared__ __align__(1024) unsigned char smem[LDS];
+  __shared__ float ml_lds[kWaves][32][2];
+  __shared__ ShareLds share_lds;
+
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
+  const int group = p.n_q_heads / p.n_kv_heads;
+  auto units_of = [&](const Lens& n) { return n.count ? (long long)row_tiles<WR>(p, n) * key_units(n) * p.n_kv_heads : 0LL; };
+  const Share sh = find_share(p, share_lds, units_of);
+  if (tid == 0) p.splits[blockIdx.x].n_pieces = 0;
+  if (sh.idle) return;
+  int s = sh.seq;
+  long long seq_base = sh.seq_base, at = sh.begin;
   Lens n = lens_of(p, s);
 
-  while (at < end) {
+  while (at < sh.end) {
     // ---- the piece: units of one row tile
     while (n.count == 0 || at >= seq_base + units_of(n)) {  // the share has another unit, so there is another sequence
       seq_base += units_of(n);
@@ -182,7 +221,7 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
     const int tile_index = (int)(rel / n_key_units), unit = (int)(rel - (long long)tile_index * n_key_units);
     const int kv_head = tile_index / n_tiles, tile = tile_index - kv_head * n_tiles;
     const long long item_end = at - unit + n_key_units;
-    const long long piece_end = min(item_end, end);
+    const long long piece_end = min(item_end, sh.end);
     const int key_begin = unit * kUnitKeys, key_end = min(kv_len, (unit + (int)(piece_end - at)) * kUnitKeys);
     const int row0 = tile * ROWS, n_rows = min(ROWS, n.count * group - row0);
     const bool whole = unit == 0 && piece_end == item_end;
@@ -194,10 +233,9 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
     const unsigned flip = c < 0 ? 0x80008000u : 0u;  // the running maximum is that of the scores: a negative factor goes into q
     c = fabsf(c);
     if (c < 1e-37f) c = 1e-37f;  // and 0 times the -infinity of a key that is not seen is no weight
+    u32x4 qraw[NSTEP];
     bf16x8 qreg[NSTEP];
     const unsigned short* qp = p.q + ((long long)(n.first + token) * p.n_q_heads + head) * D + 8 * half;
-#pragma unroll
-    for (int st = 0; st < NSTEP; ++st) qreg[st] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + 16 * st) ^ flip);
 
     f32x16 o[NDB];
     float m = kNeg, l = 0.f;
@@ -206,53 +244,20 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
 
-    // ---- keys: sub-tiles wk, wk + WK, ... of the piece
     const int* table = p.block_tables + (long long)s * p.max_blocks;
     const int last_block = (kv_len - 1) / kBlock;
-    const long long head_bytes = 16 * D * ESZ;
     const int pr = perm32(c32);
-    const int k_off = (half * 16 + (pr & 15)) * 8 * ESZ, v_off = (half * D + pr) * 8 * ESZ;
-    Chunk k[NSTEP], v[NSTEP];
-    auto block_at = [&](int key, int b) { return (long long)table[min(key / kBlock + b, last_block)]; };
-    auto load_k = [&](long long b0, long long b1) {
-      const unsigned char* g = p.k_pool + (((pr >> 4) ? b1 : b0) * p.n_kv_heads + kv_head) * head_bytes + k_off;
-#pragma unroll
-      for (int st = 0; st < NSTEP; ++st) k[st] = *reinterpret_cast<const Chunk*>(g + st * 256 * ESZ);
-    };
-    auto load_v = [&](long long b0, long long b1) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const unsigned char* g = p.v_pool + ((t ? b1 : b0) * p.n_kv_heads + kv_head) * head_bytes + v_off;
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) v[t * NDB + db] = *reinterpret_cast<const Chunk*>(g + db * 256 * ESZ);
-      }
-    };
-    auto operand = [&](Chunk x) {
-      if constexpr (FP8) return fp8x8_to_bf16x8(x);
-      else return x;
-    };
-    int key = key_begin + 32 * wk;
-    if (key < key_end) {
-      const long long b0 = block_at(key, 0), b1 = block_at(key, 1);
-      load_k(b0, b1);
-      load_v(b0, b1);
-    }
-    for (; key < key_end; key += 32 * WK) {
-      const int next = key + 32 * WK;
-      long long b0 = 0, b1 = 0;
-      if (next < key_end) b0 = block_at(next, 0), b1 = block_at(next, 1);
-      f32x16 sc;
+
+    // ---- a sub-tile of 32 keys
+    auto scores = [&](const u32x4 (&kop)[NSTEP], f32x16& sc) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
-      for (int st = 0; st < NSTEP; ++st)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(operand(k[st])), qreg[st], sc, 0, 0, 0);
-      if (next < key_end) load_k(b0, b1);
-      const bool tail = key + 32 > n.prefix;
-      unsigned seen = ~0u;
-      if (tail) {
-        seen = visible_bits(p, n, token, key);
-        const unsigned own = seen >> (8 * half);
+      for (int st = 0; st < NSTEP; ++st) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kop[st]), qreg[st], sc, 0, 0, 0);
+    };
+    auto weights = [&](f32x16& sc, int key, u32x4 (&pp)[2]) {
+      if (key + 32 > n.prefix) {
+        const unsigned own = visible_bits(p, n, token, key) >> (8 * half);
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[i] = own >> (16 * (i >> 3) + (i & 7)) & 1 ? sc[i] : -__builtin_inff();
       }
@@ -271,23 +276,35 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
           for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
         m = m_new;
       }
-      u32x4 pp[2];
       l += softmax_exp_part(sc, c, m, pp);
-      u32x4 vop[NSTEP];
-#pragma unroll
-      for (int x = 0; x < NSTEP; ++x) vop[x] = operand(v[x]);
+    };
+    auto sums = [&](u32x4 (&vop)[NSTEP], const u32x4 (&pp)[2], int key) {
       bool odd = false;
-      if (tail) {
+      if (key + 32 > n.prefix) {
         if (key + 32 > kv_len) {
 #pragma unroll
           for (int x = 0; x < NSTEP; ++x) vop[x] = zero_tail(vop[x], key + 16 * (x / NDB) + 8 * half, kv_len);
         }
+        bool mine = false;
 #pragma unroll
-        for (int x = 0; x < NSTEP; ++x) odd |= not_finite(vop[x]);
+        for (int x = 0; x < NSTEP; ++x) mine |= not_finite(vop[x]);
+        odd = __builtin_amdgcn_ballot_w64(mine) != 0;
+        if (odd) {
+#pragma unroll
+          for (int x = 0; x < NSTEP; ++x) vop[x] = finite_only(vop[x]);
+        }
       }
-      if (tail && __builtin_amdgcn_ballot_w64(odd) != 0) {
-        // An infinite or NaN value that some rows do not see: 0 times it would be NaN, so their sums leave the key out.
-        for (int b = 0; b < 32; ++b) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vop[t * NDB + db]), as_bf16x8(pp[t]), o[db], 0, 0, 0);
+      if (odd) {
+        // Infinite and NaN values are added to the rows that see their key, one after the other: in the product, 0 times such a value
+        // would be NaN in the others.
+        const unsigned seen = visible_bits(p, n, token, key);
+#pragma unroll 1
+        for (int b = 0; b < 32 && key + b < kv_len; ++b) {
           const int x = (b >> 4) * 4 + ((b & 7) >> 1);
           unsigned word = 0;
 #pragma unroll
@@ -295,8 +312,8 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
           word = __shfl(word, c32 + 32 * (b >> 3 & 1));
           const float weight = __uint_as_float(b & 1 ? word & 0xffff0000u : word << 16);
           const int pos = key + b;
-          if (pos >= kv_len) break;
-          const unsigned char* g = p.v_pool + (block_at(pos, 0) * p.n_kv_heads + kv_head) * head_bytes + (pos % kBlock / 8 * D * 8 + pos % 8) * ESZ;
+          const unsigned char* g =
+              p.v_pool + ((long long)table[pos / kBlock] * p.n_kv_heads + kv_head) * BLKB + (pos % kBlock / 8 * D * 8 + pos % 8) * ESZ;
 #pragma unroll
           for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -305,28 +322,196 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
               float value;
               if constexpr (FP8) value = __builtin_amdgcn_cvt_f32_fp8((int)g[d * 8], 0);
               else value = __uint_as_float((unsigned)reinterpret_cast<const unsigned short*>(g)[d * 8] << 16);
-              o[db][i] = seen >> b & 1 ? __builtin_fmaf(weight, value, o[db][i]) : o[db][i];
-              asm volatile("" : "+v"(o[db][i]) : : "memory");  // one value after the other: no registers for a path that is hardly ever taken
+              const bool add = (seen >> b & 1) && (__float_as_uint(value) & 0x7f800000u) == 0x7f800000u;
+              o[db][i] = add ? __builtin_fmaf(weight, value, o[db][i]) : o[db][i];
+              asm volatile("" : "+v"(o[db][i]) : : "memory");  // one at a time: no registers for a path that is hardly ever taken
             }
         }
-      } else {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int db = 0; db < NDB; ++db)
-            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vop[t * NDB + db]), as_bf16x8(pp[t]), o[db], 0, 0, 0);
       }
-      if (next < key_end) load_v(b0, b1);
+    };
+    auto load_q = [&]() {
+#pragma unroll
+      for (int st = 0; st < NSTEP; ++st) qraw[st] = *reinterpret_cast<const u32x4*>(qp + 16 * st);
+    };
+    auto pin_q = [&]() {  // waits for q here
+#pragma unroll
+      for (int st = 0; st < NSTEP; ++st) {
+        asm volatile("" : "+v"(qraw[st]));
+        qreg[st] = as_bf16x8(qraw[st] ^ flip);
+      }
+    };
+
+    if constexpr (STAGED) {
+      // ---- tiles of kUnitKeys keys, one in LDS, the next in registers; piece x of a block is 16 bytes of the image in LDS
+      static_assert(WK <= kUnitKeys / 32, "a sub-tile for every group of waves");
+      constexpr int PIECES = 4 * D;                          // of K and V of a block: 8 elements each
+      constexpr int PER = kUnitKeys / kBlock * PIECES / kThreads;  // of a thread
+      using Piece = std::conditional_t<FP8, u32x2, u32x4>;
+      Piece r[PER];
+      auto fetch = [&](int key) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int x = i * kThreads + tid, b = x / PIECES, in = x % PIECES;
+          const long long block = table[min(key / kBlock + __builtin_amdgcn_readfirstlane(b), last_block)];
+          const unsigned char* pool = __builtin_amdgcn_readfirstlane(in / (PIECES / 2)) ? p.v_pool : p.k_pool;
+          r[i] = *reinterpret_cast<const Piece*>(pool + (block * p.n_kv_heads + kv_head) * BLKB + in % (PIECES / 2) * (8 * ESZ));
+        }
+      };
+      auto put = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          u32x4 w;
+          if constexpr (FP8) w = fp8x8_to_bf16x8(r[i]);
+          else w = r[i];
+          *reinterpret_cast<u32x4*>(smem + buffer * TILE + (i * kThreads + tid) * 16) = w;
+        }
+      };
+      load_q();
+      fetch(key_begin);
+      pin_q();
+      int buffer = 0;
+      for (int key0 = key_begin; key0 < key_end; key0 += kUnitKeys, buffer ^= 1) {
+        put(buffer);
+        if (key0 + kUnitKeys < key_end) fetch(key0 + kUnitKeys);
+        __syncthreads();
+#pragma unroll
+        for (int sub = 0; sub < kUnitKeys / 32; ++sub) {
+          const int key = key0 + 32 * sub;
+          if (sub % WK != wk || key >= key_end) continue;
+          const unsigned char* tile_lds = smem + buffer * TILE + 2 * sub * (PIECES * 16);
+          u32x4 kop[NSTEP], vop[NSTEP], pp[2];
+          f32x16 sc;
+#pragma unroll
+          for (int st = 0; st < NSTEP; ++st)
+            kop[st] = *reinterpret_cast<const u32x4*>(tile_lds + (pr >> 4) * (PIECES * 16) + ((2 * st + half) * 16 + (pr & 15)) * 16);
+          scores(kop, sc);
+          weights(sc, key, pp);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+              vop[t * NDB + db] = *reinterpret_cast<const u32x4*>(tile_lds + t * (PIECES * 16) + PIECES * 8 + (half * D + 32 * db + pr) * 16);
+          sums(vop, pp, key);
+        }
+      }
+      if constexpr (WK > 1) __syncthreads();  // results take the place of the tiles
+    } else {
+      // ---- sub-tiles wk, wk + WK, ... of the piece; table entries of the next 32 of them in one register, two lanes each
+      int bt_reg = 0;
+      auto load_table = [&](int j0) {
+        const int u = wk + WK * (j0 + (lane >> 1));
+        bt_reg = table[min((key_begin + 32 * u) / kBlock + (lane & 1), last_block)];
+      };
+      auto pin_table = [&]() { asm volatile("" : "+v"(bt_reg)); };
+      const int n_sub = (key_end - key_begin + 31) / 32;
+      const int n_iter = n_sub > wk ? (n_sub - wk + WK - 1) / WK : 0;
+      lds_byte* wl = (lds_byte*)smem + wave * WAVE_LDS;
+      const unsigned wl_addr = (unsigned)(unsigned long long)wl;
+      load_table(0);
+      load_q();
+      pin_table();
+      if constexpr (!FP8) {
+        const unsigned rd = wl_addr + lane * 16;  // each lane reads back the chunks that it fetched
+        const int k_off = (half * 16 + (pr & 15)) * 16, v_off = (half * D + pr) * 16;
+        auto issue_k = [&](int j) {
+          const long long b0 = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31)), b1 = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + 1);
+          const unsigned char* g = p.k_pool + (((pr >> 4) ? b1 : b0) * p.n_kv_heads + kv_head) * BLKB + k_off;
+#pragma unroll
+          for (int st = 0; st < NSTEP; ++st) __builtin_amdgcn_global_load_lds(g + st * 512, wl + st * 1024, 16, 0, 0);
+        };
+        auto issue_v = [&](int j) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const long long b = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + t);
+            const unsigned char* g = p.v_pool + (b * p.n_kv_heads + kv_head) * BLKB + v_off;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) __builtin_amdgcn_global_load_lds(g + db * 512, wl + (NSTEP + t * NDB + db) * 1024, 16, 0, 0);
+          }
+        };
+        if (n_iter > 0) {
+          issue_k(0);
+          issue_v(0);
+        }
+        pin_q();
+        for (int j = 0; j < n_iter; ++j) {
+          const int key = key_begin + 32 * (wk + WK * j);
+          const bool more = j + 1 < n_iter;
+          u32x4 kop[NSTEP], vop[NSTEP], pp[2];
+          f32x16 sc;
+          wait_vmcnt<NSTEP>();  // K(j) has landed; the V(j) loads behind it may still fly
+          lds_read_planes<NSTEP>(kop, rd);
+          scores(kop, sc);
+          if (more) {
+            if (((j + 1) & 31) == 0) {
+              load_table(j + 1);
+              pin_table();
+            }
+            issue_k(j + 1);
+          }
+          weights(sc, key, pp);
+          if (more) wait_vmcnt<NSTEP>();
+          else wait_vmcnt<0>();  // V(j) has landed
+          lds_read_planes<NSTEP>(vop, rd + NSTEP * 1024);
+          sums(vop, pp, key);
+          if (more) issue_v(j + 1);
+        }
+      } else {
+        // The two blocks of a sub-tile are copied whole (K: the second image 128 bytes further, so that the halves of a read hit
+        // different banks), the operands' 8-byte chunks picked out of the images and converted.  Two sets.
+        constexpr int NIB = BLKB / 1024, NIK = 2 * NIB, KSET = 2 * BLKB + 128, SET = KSET + 2 * BLKB;
+        static_assert(2 * SET <= WAVE_LDS, "two sets per wave");
+        const unsigned k_rd = wl_addr + (pr >> 4) * (BLKB + 128) + (half * 16 + (pr & 15)) * 8, v_rd = wl_addr + KSET + (half * D + pr) * 8;
+        auto issue = [&](int j) {
+          if (j && (j & 31) == 0) {
+            load_table(j);
+            pin_table();
+          }
+          lds_byte* set = wl + (j & 1) * SET;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {  // K of both blocks, then V
+            const long long b = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + (x & 1));
+            const unsigned char* g = (x < 2 ? p.k_pool : p.v_pool) + (b * p.n_kv_heads + kv_head) * BLKB + lane * 16;
+#pragma unroll
+            for (int i = 0; i < NIB; ++i)
+              __builtin_amdgcn_global_load_lds(g + i * 1024, set + (x < 2 ? x * (BLKB + 128) : KSET + (x - 2) * BLKB) + i * 1024, 16, 0, 0);
+          }
+        };
+        if (n_iter > 0) issue(0);
+        if (n_iter > 1) issue(1);
+        pin_q();
+        for (int j = 0; j < n_iter; ++j) {
+          const int key = key_begin + 32 * (wk + WK * j);
+          const bool more = j + 1 < n_iter;  // sub-tile j + 1 has been requested
+          u32x4 kop[NSTEP], vop[NSTEP], pp[2];
+          u32x2 codes[NSTEP];
+          f32x16 sc;
+          if (more) wait_vmcnt<3 * NIK>();
+          else wait_vmcnt<NIK>();  // K(j) has landed
+          if constexpr (NSTEP == 8) lds_read8_b64<0, 256, 512, 768, 1024, 1280, 1536, 1792>(codes, k_rd + (j & 1) * SET);
+          else lds_read4_b64<0, 256, 512, 768>(codes, k_rd + (j & 1) * SET);
+#pragma unroll
+          for (int x = 0; x < NSTEP; ++x) kop[x] = fp8x8_to_bf16x8(codes[x]);
+          scores(kop, sc);
+          weights(sc, key, pp);
+          if (more) wait_vmcnt<2 * NIK>();
+          else wait_vmcnt<0>();  // V(j) has landed
+          if constexpr (NSTEP == 8) lds_read8_b64<0, 256, 512, 768, BLKB, BLKB + 256, BLKB + 512, BLKB + 768>(codes, v_rd + (j & 1) * SET);
+          else lds_read4_b64<0, 256, BLKB, BLKB + 256>(codes, v_rd + (j & 1) * SET);
+          if (j + 2 < n_iter) issue(j + 2);  // the set is free again
+#pragma unroll
+          for (int x = 0; x < NSTEP; ++x) vop[x] = fp8x8_to_bf16x8(codes[x]);
+          sums(vop, pp, key);
+        }
+      }
     }
     l = pair_sum(l);
 
     // ---- results: final rows, or a slot of the partial results
-    const int slot = 2 * share + (unit == 0 ? 1 : 0);
-    float* part = p.partials + (long long)slot * kSlotFloats<D, WR>;
+    float* part = p.partials + (long long)(2 * sh.index + (unit == 0 ? 1 : 0)) * kSlotFloats<D, WR>;
     const float v_factor = FP8 ? p.v_scale[kv_head] : 1.0f;
-    auto store_final = [&](int r, int d, float (&x)[8], float sum) {  // 8 dims of row r of the tile
+    auto store_final = [&](int r, int d, const float (&x)[8], float sum) {  // 8 dims of row r of the tile
       const int tok = (row0 + r) / group, h = kv_head * group + (row0 + r) - tok * group;
-      float f = v_factor / sum;
+      const float f = v_factor / sum;
       u32x4 w;
       if (sum == 0.f && sees_nothing(p, n, tok)) {
         w = u32x4{0, 0, 0, 0};
@@ -360,13 +545,15 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
           part[ROWS * D + 2 * r + 1] = l;
         }
       }
+      __syncthreads();  // before the next piece's first tile: LDS is still being read
     } else {
-      float* mine_o = o_lds + (wave * 32 + c32) * PITCH;
+      constexpr int PITCH = STAGED ? RESULT : WAVE_LDS;
+      float* mine = reinterpret_cast<float*>(smem + wave * PITCH) + c32 * D;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
         for (int h = 0; h < 4; ++h)
-          *reinterpret_cast<f32x4*>(mine_o + 32 * db + 16 * (h >> 1) + 8 * half + 4 * (h & 1)) =
+          *reinterpret_cast<f32x4*>(mine + ((8 * db + 4 * (h >> 1) + 2 * half + (h & 1)) ^ (c32 & SWZ)) * 4) =
               f32x4{o[db][4 * h], o[db][4 * h + 1], o[db][4 * h + 2], o[db][4 * h + 3]};
       if (half == 0) {
         ml_lds[wave][c32][0] = m * c;
@@ -383,8 +570,9 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
         for (int w = 0; w < WK; ++w) {
           const float f = __builtin_amdgcn_exp2f(ml_lds[w0 + w][rr][0] - top);
           sum = __builtin_fmaf(f, ml_lds[w0 + w][rr][1], sum);
-          const float* from = o_lds + ((w0 + w) * 32 + rr) * PITCH + d;
-          const f32x4 a = *reinterpret_cast<const f32x4*>(from), b = *reinterpret_cast<const f32x4*>(from + 4);
+          const float* from = reinterpret_cast<const float*>(smem + (w0 + w) * PITCH) + rr * D;
+          const f32x4 a = *reinterpret_cast<const f32x4*>(from + ((d / 4) ^ (rr & SWZ)) * 4);
+          const f32x4 b = *reinterpret_cast<const f32x4*>(from + ((d / 4 + 1) ^ (rr & SWZ)) * 4);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             acc[e] = __builtin_fmaf(f, a[e], acc[e]);
@@ -404,9 +592,9 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
       __syncthreads();
     }
     if (unit == 0 && !whole && tid == 0) {
-      int last = share + 1;
-      while ((last + 1) * total / active < item_end) ++last;
-      p.splits[blockIdx.x] = Split{last - share + 1, share, n_rows, row0, kv_head, n.first, n.prefix, n.count};
+      int last = sh.index + 1;
+      while ((last + 1) * sh.total / sh.active < item_end) ++last;
+      p.splits[blockIdx.x] = Split{last - sh.index + 1, sh.index, n_rows, row0, kv_head, n.first, n.prefix, n.count};
     }
     at = piece_end;
   }
@@ -449,7 +637,7 @@ size_t split_bytes(int n_cus) { return ((size_t)n_cus * sizeof(Split) + 255) / 2
 
 template <int D, bool FP8, int WR>
 int launch(const TreeParams& p, int n_cus, hipStream_t stream) {
-  hipLaunchKernelGGL((attn_tree_kernel<D, FP8, WR>), dim3(n_cus), dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL((attn_tree_kernel<D, FP8, WR, (WR >= 4)>), dim3(n_cus), dim3(kThreads), 0, stream, p);
   if (hipGetLastError() != hipSuccess) return CRONUS_ERR_HIP;
   hipLaunchKernelGGL((merge_kernel<D, FP8, WR>), dim3(n_cus, 32 * WR * D / 1024), dim3(256), 0, stream, p);
   return hipGetLastError() == hipSuccess ? CRONUS_OK : CRONUS_ERR_HIP;

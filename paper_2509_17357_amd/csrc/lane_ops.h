@@ -13,6 +13,8 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
 constexpr float kLazyLog2 = 8.0f;  // slack of the running reference of the online softmax, in bits
 constexpr float kNeg = -1.0e30f;  // initial running maximum: finite, so that differences of maxima stay finite
 
@@ -80,6 +82,68 @@ __device__ __forceinline__ float softmax_exp_part(const f32x16& s, float c, floa
       sum = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, sum, false);
     }
   return sum;
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
+}
+
+// LDS reads of data that arrived by global_load_lds are written as asm, so that the
+// waits on those loads are the explicit vmcnt waits of the pipelines and nothing coarser
+// (the compiler would wait for every DMA in flight before any LDS read).  The reads and
+// the wait for them form ONE asm statement: its outputs are valid when it ends, so no
+// register copy the compiler may insert afterwards can see a value that has not arrived.
+template <int O0, int O1, int O2, int O3>
+__device__ __forceinline__ void lds_read4(u32x4& x0, u32x4& x1, u32x4& x2, u32x4& x3, unsigned addr) {
+  asm volatile(
+      "ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%6\n\t"
+      "ds_read_b128 %2, %4 offset:%7\n\tds_read_b128 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(x0), "=&v"(x1), "=&v"(x2), "=&v"(x3)
+      : "v"(addr), "i"(O0), "i"(O1), "i"(O2), "i"(O3)
+      : "memory");
+}
+template <int O0, int O1, int O2, int O3, int O4, int O5, int O6, int O7>
+__device__ __forceinline__ void lds_read8(u32x4 (&x)[8], unsigned addr) {
+  asm volatile(
+      "ds_read_b128 %0, %8 offset:%9\n\tds_read_b128 %1, %8 offset:%10\n\t"
+      "ds_read_b128 %2, %8 offset:%11\n\tds_read_b128 %3, %8 offset:%12\n\t"
+      "ds_read_b128 %4, %8 offset:%13\n\tds_read_b128 %5, %8 offset:%14\n\t"
+      "ds_read_b128 %6, %8 offset:%15\n\tds_read_b128 %7, %8 offset:%16\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+      : "v"(addr), "i"(O0), "i"(O1), "i"(O2), "i"(O3), "i"(O4), "i"(O5), "i"(O6), "i"(O7)
+      : "memory");
+}
+
+// Read the NOPS 1-KiB operand planes of this lane (plane n at addr + 1024 n).
+template <int NOPS>
+__device__ __forceinline__ void lds_read_planes(u32x4 (&x)[NOPS], unsigned addr) {
+  static_assert(NOPS == 4 || NOPS == 8, "D = 64 or 128");
+  if constexpr (NOPS == 8) lds_read8<0, 1024, 2048, 3072, 4096, 5120, 6144, 7168>(x, addr);
+  else lds_read4<0, 1024, 2048, 3072>(x[0], x[1], x[2], x[3], addr);
+}
+
+// Operand chunks of 8 bytes picked out of a block image in LDS (fp8 codes).
+template <int O0, int O1, int O2, int O3, int O4, int O5, int O6, int O7>
+__device__ __forceinline__ void lds_read8_b64(u32x2 (&x)[8], unsigned addr) {
+  asm volatile(
+      "ds_read_b64 %0, %8 offset:%9\n\tds_read_b64 %1, %8 offset:%10\n\t"
+      "ds_read_b64 %2, %8 offset:%11\n\tds_read_b64 %3, %8 offset:%12\n\t"
+      "ds_read_b64 %4, %8 offset:%13\n\tds_read_b64 %5, %8 offset:%14\n\t"
+      "ds_read_b64 %6, %8 offset:%15\n\tds_read_b64 %7, %8 offset:%16\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+      : "v"(addr), "i"(O0), "i"(O1), "i"(O2), "i"(O3), "i"(O4), "i"(O5), "i"(O6), "i"(O7)
+      : "memory");
+}
+template <int O0, int O1, int O2, int O3>
+__device__ __forceinline__ void lds_read4_b64(u32x2 (&x)[4], unsigned addr) {
+  asm volatile(
+      "ds_read_b64 %0, %4 offset:%5\n\tds_read_b64 %1, %4 offset:%6\n\t"
+      "ds_read_b64 %2, %4 offset:%7\n\tds_read_b64 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+      : "v"(addr), "i"(O0), "i"(O1), "i"(O2), "i"(O3)
+      : "memory");
 }
 
 }  // namespace cronus
