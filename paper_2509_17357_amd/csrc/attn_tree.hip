@@ -348,11 +348,20 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
       constexpr int PER = kUnitKeys / kBlock * PIECES / kThreads;  // of a thread
       using Piece = std::conditional_t<FP8, u32x2, u32x4>;
       Piece r[PER];
-      auto fetch = [&](int key) {
+      // Table entries of 16 tiles in one register, a lane each, and of the 16 after them: an entry is there when its block is
+      // requested (loaded with each tile, they cost it their round trip).
+      constexpr int kAhead = 64 * kBlock / kUnitKeys;
+      int entries = 0, entries_next = 0;
+      auto load_table = [&](int j) { return table[min(key_begin / kBlock + j * (kUnitKeys / kBlock) + lane, last_block)]; };
+      auto fetch = [&](int j) {  // tile j of the piece
+        if (j && j % kAhead == 0) {
+          entries = entries_next;
+          entries_next = load_table(j + kAhead);
+        }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-          const int x = i * kThreads + tid, b = x / PIECES, in = x % PIECES;
-          const long long block = table[min(key / kBlock + __builtin_amdgcn_readfirstlane(b), last_block)];
+          const int x = i * kThreads + tid, b = __builtin_amdgcn_readfirstlane(x / PIECES), in = x % PIECES;
+          const long long block = __builtin_amdgcn_readlane(entries, (j % kAhead) * (kUnitKeys / kBlock) + b);
           const unsigned char* pool = __builtin_amdgcn_readfirstlane(in / (PIECES / 2)) ? p.v_pool : p.k_pool;
           r[i] = *reinterpret_cast<const Piece*>(pool + (block * p.n_kv_heads + kv_head) * BLKB + in % (PIECES / 2) * (8 * ESZ));
         }
@@ -366,13 +375,16 @@ __global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
           *reinterpret_cast<u32x4*>(smem + buffer * TILE + (i * kThreads + tid) * 16) = w;
         }
       };
+      entries = load_table(0);
       load_q();
-      fetch(key_begin);
+      if (key_end - key_begin > kAhead * kUnitKeys) entries_next = load_table(kAhead);
+      fetch(0);
       pin_q();
-      int buffer = 0;
-      for (int key0 = key_begin; key0 < key_end; key0 += kUnitKeys, buffer ^= 1) {
+      const int n_keys_tiles = (key_end - key_begin + kUnitKeys - 1) / kUnitKeys;
+      for (int j = 0; j < n_keys_tiles; ++j) {
+        const int key0 = key_begin + j * kUnitKeys, buffer = j & 1;
         put(buffer);
-        if (key0 + kUnitKeys < key_end) fetch(key0 + kUnitKeys);
+        if (j + 1 < n_keys_tiles) fetch(j + 1);
         __syncthreads();
 #pragma unroll
         for (int sub = 0; sub < kUnitKeys / 32; ++sub) {

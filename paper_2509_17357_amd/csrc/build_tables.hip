@@ -6,8 +6,9 @@
 // A new block holds at least one new token (h >= ceil(L / 16)), so whoever maps the first token of a block that the
 // sequence did not hold also writes the table entry: one pass over the tokens fills both.
 //
-// Two launches: plan_kernel, one work-group, checks the lengths, sums them and returns the blocks of ended sequences to the
-// free stack; map_kernel writes table entries and slots, and is ordered behind it because it reads what that one returned.
+// plan_kernel, one work-group, checks the lengths, sums them and returns the blocks of ended sequences to the free stack;
+// map_kernel writes table entries and slots, and is ordered behind it because it reads what that one returned.  A batch of few
+// sequences and tokens is mapped by plan_kernel itself: one launch, and the sums are still in LDS.
 #include <hip/hip_runtime.h>
 
 #include "cronus_internal.h"
@@ -17,6 +18,8 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kMapThreads = 256, kMapTokens = 4;  // tokens of a thread of map_kernel
+constexpr int kFewTokens = 4096;                  // of a batch that plan_kernel maps, of at most kPlanThreads sequences
+constexpr int kMapSeqs = 4096;                    // sequences whose offsets map_kernel searches in LDS
 
 struct TableParams {
   cronus_paged_tables t;
@@ -62,87 +65,29 @@ __device__ __forceinline__ Sums from_lane(Sums a, int lane) {
 
 // Sum of the values of the threads before this one, and of all (*total).  lds: one entry for each wave.
 __device__ __forceinline__ Sums scan_threads(Sums x, Sums* lds, Sums* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   Sums incl = x;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const Sums y = from_lane(incl, lane - d < 0 ? lane : lane - d);
     if (lane >= d) incl = plus(incl, y);
   }
-  if (lane == 63) lds[wave] = incl;
-  __syncthreads();
-  Sums before{0, 0, 0}, all{0, 0, 0};
+  if (waves == 1) {
+    *total = from_lane(incl, 63);
+  } else {
+    if (lane == 63) lds[wave] = incl;
+    __syncthreads();
+    Sums before{0, 0, 0}, all{0, 0, 0};
 #pragma unroll 2
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
-    if (w == wave) before = all;
-    all = plus(all, lds[w]);
-  }
-  __syncthreads();
-  *total = all;
-  return {before.tokens + incl.tokens - x.tokens, before.need + incl.need - x.need, before.back + incl.back - x.back};
-}
-
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(TableParams p) {
-  __shared__ Sums lds[kPlanThreads / 64];
-  __shared__ int first_bad;
-  const int t = threadIdx.x;
-  if (t == 0) first_bad = 0x7fffffff;
-  __syncthreads();
-  Sums mine{0, 0, 0}, total;
-  for (int s = t; s < p.n_seqs; s += kPlanThreads) {
-    const Ask a = ask_of(p, s);
-    if (!a.ok) {
-      atomicMin(&first_bad, s);
-      break;
+    for (int w = 0; w < waves; ++w) {
+      if (w == wave) before = all;
+      all = plus(all, lds[w]);
     }
-    mine = plus(mine, Sums{a.add, a.need, a.back});
+    __syncthreads();
+    *total = all;
+    incl = plus(incl, before);
   }
-  scan_threads(mine, lds, &total);
-  const int bad = first_bad;
-  const long long count = *p.t.free_count;
-  int status = CRONUS_TABLES_OK;
-  if (bad != 0x7fffffff || count < 0 || count + total.back > p.t.free_capacity) status = CRONUS_TABLES_BAD_LENGTHS;
-  else if (total.need > count + total.back) status = CRONUS_TABLES_NO_BLOCKS;
-  else if (total.tokens > p.max_tokens) status = CRONUS_TABLES_TOO_MANY_TOKENS;
-  const bool ok = status == CRONUS_TABLES_OK;
-  __syncthreads();  // every thread has read free_count, which free_count_out may be
-  if (t == 0) {
-    *p.t.free_count_out = (int)(ok ? count + total.back - total.need : count);
-    p.cu_tokens[0] = 0;
-    p.cu_blocks[0] = 0;
-    p.report[0] = status;
-    p.report[1] = (int)min(total.tokens, 0x7fffffffLL);
-    p.report[2] = (int)min(total.need, 0x7fffffffLL);
-    p.report[3] = bad != 0x7fffffff ? bad : -1;
-  }
-  Sums carry{0, 0, 0};
-  for (int s0 = 0; s0 < p.n_seqs; s0 += kPlanThreads) {
-    const int s = s0 + t;
-    Ask a{};
-    if (s < p.n_seqs) {
-      if (ok) a = ask_of(p, s);
-      else a.start = p.kv_lens[s], a.held = p.t.held[s];
-    }
-    Sums part;
-    const Sums before = plus(carry, scan_threads(Sums{a.add, a.need, a.back}, lds, &part));
-    carry = plus(carry, part);
-    if (s < p.n_seqs) {
-      p.cu_tokens[s + 1] = (int)(before.tokens + a.add);
-      p.cu_blocks[s + 1] = (int)(before.need + a.need);
-      p.start_pos[s] = a.start;
-      p.t.held_out[s] = a.held - a.back + a.need;
-    }
-    // The blocks of this wave's ended sequences, one sequence after the other, 64 entries at a time.
-    unsigned long long ended = __builtin_amdgcn_ballot_w64(a.back > 0);
-    while (ended) {
-      const int from = __builtin_ctzll(ended);
-      ended &= ended - 1;
-      const int n = __shfl(a.back, from);
-      const long long at = count + __shfl(before.back, from);
-      const int* row = p.t.block_tables + (long long)(s - (t & 63) + from) * p.t.max_blocks_per_seq;
-      for (int i = t & 63; i < n; i += 64) p.t.free_blocks[at + i] = row[i];
-    }
-  }
+  return {incl.tokens - x.tokens, incl.need - x.need, incl.back - x.back};
 }
 
 // Last s in [0, n_seqs) with cu[s] <= token; sequences without tokens are passed over.
@@ -156,15 +101,141 @@ __device__ __forceinline__ int sequence_of(const int* cu, int n_seqs, int token)
   return lo;
 }
 
+// Slot of the token at position pos of a sequence (its table row, blocks that it held, blocks granted before it); the table entry of a
+// granted block is written with the block's first token.  top: entries of the free stack before blocks were taken.
+__device__ __forceinline__ long long map_token(const TableParams& p, int* row, int pos, int old_held, int grant, long long top) {
+  const int column = pos / kBlock;
+  const bool fresh = column >= old_held;
+  const int* from = fresh ? p.t.free_blocks + (top - 1 - grant - (column - old_held)) : row + column;
+  const int block = *from;
+  if (fresh && pos % kBlock == 0) row[column] = block;
+  return (long long)block * kBlock + pos % kBlock;
+}
+
+struct Ended {
+  int seq, n;
+  long long at;  // place of its blocks on the stack
+};
+
+template <bool MAPS>
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(TableParams p) {
+  __shared__ Sums lds[kPlanThreads / 64];
+  __shared__ Ended ended[kPlanThreads];
+  __shared__ int n_ended, first_bad;
+  __shared__ int map_cu[MAPS ? kPlanThreads + 1 : 1], map_start[MAPS ? kPlanThreads : 1], map_held[MAPS ? kPlanThreads : 1], map_grant[MAPS ? kPlanThreads : 1];
+  const int t = threadIdx.x, threads = blockDim.x, lane = t & 63;
+  const long long count = *p.t.free_count;
+  if (t == 0) first_bad = 0x7fffffff, n_ended = 0;
+  __syncthreads();
+  // One round of the threads holds the whole batch, or the sums come first and the batch is read again.
+  const bool once = p.n_seqs <= threads;
+  Ask a{};
+  Sums mine{0, 0, 0}, total;
+  for (int s = t; s < p.n_seqs; s += threads) {
+    a = ask_of(p, s);
+    if (!a.ok) {
+      atomicMin(&first_bad, s);
+      break;
+    }
+    mine = plus(mine, Sums{a.add, a.need, a.back});
+  }
+  Sums before = scan_threads(mine, lds, &total);
+  __syncthreads();  // first_bad; and every thread has read free_count, which free_count_out may be
+  const int bad = first_bad;
+  int status = CRONUS_TABLES_OK;
+  if (bad != 0x7fffffff || count < 0 || count + total.back > p.t.free_capacity) status = CRONUS_TABLES_BAD_LENGTHS;
+  else if (total.need > count + total.back) status = CRONUS_TABLES_NO_BLOCKS;
+  else if (total.tokens > p.max_tokens) status = CRONUS_TABLES_TOO_MANY_TOKENS;
+  const bool ok = status == CRONUS_TABLES_OK;
+  if (t == 0) {
+    *p.t.free_count_out = (int)(ok ? count + total.back - total.need : count);
+    p.cu_tokens[0] = 0;
+    p.cu_blocks[0] = 0;
+    p.report[0] = status;
+    p.report[1] = (int)min(total.tokens, 0x7fffffffLL);
+    p.report[2] = (int)min(total.need, 0x7fffffffLL);
+    p.report[3] = bad != 0x7fffffff ? bad : -1;
+  }
+  Sums carry{0, 0, 0};
+  for (int s0 = 0; s0 < p.n_seqs; s0 += threads) {
+    const int s = s0 + t;
+    if (!ok) {
+      a = Ask{};
+      before = carry;
+      if (s < p.n_seqs) a.start = p.kv_lens[s], a.held = p.t.held[s];
+    } else if (!once) {
+      a = Ask{};
+      if (s < p.n_seqs) a = ask_of(p, s);
+      Sums part;
+      before = plus(carry, scan_threads(Sums{a.add, a.need, a.back}, lds, &part));
+      carry = plus(carry, part);
+    }
+    if (s < p.n_seqs) {
+      p.cu_tokens[s + 1] = (int)(before.tokens + a.add);
+      p.cu_blocks[s + 1] = (int)(before.need + a.need);
+      p.start_pos[s] = a.start;
+      p.t.held_out[s] = a.held - a.back + a.need;
+      if constexpr (MAPS) {
+        map_cu[s] = (int)before.tokens;
+        map_start[s] = a.start;
+        map_held[s] = a.held;
+        map_grant[s] = (int)before.need;
+      }
+    }
+    if (!ok || total.back == 0) continue;
+    // The blocks of ended sequences: a list of them, and a wave for each, whose lanes request up to kAhead entries before they
+    // store the first (one at a time, 64 of 256 sequences with 260 blocks each took 20 us).
+    if (a.back > 0) ended[atomicAdd(&n_ended, 1)] = Ended{s, a.back, count + before.back};
+    __syncthreads();
+    const int listed = n_ended;
+    for (int x = t >> 6; x < listed; x += threads >> 6) {
+      const Ended e = ended[x];
+      const int* row = p.t.block_tables + (long long)e.seq * p.t.max_blocks_per_seq;
+      constexpr int kAhead = 8;
+      for (int i0 = lane; i0 < e.n; i0 += 64 * kAhead) {
+        int b[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) b[k] = i0 + 64 * k < e.n ? row[i0 + 64 * k] : 0;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if (i0 + 64 * k < e.n) p.t.free_blocks[e.at + i0 + 64 * k] = b[k];
+      }
+    }
+    __syncthreads();
+    if (t == 0) n_ended = 0;
+    __syncthreads();
+  }
+  if constexpr (MAPS) {
+    if (!ok) return;
+    const int tokens = (int)total.tokens;
+    const long long top = count + total.back;
+    __syncthreads();  // the offsets in LDS, and what this work-group returned to the stack
+#pragma unroll 4
+    for (int token = t; token < tokens; token += threads) {
+      const int s = sequence_of(map_cu, p.n_seqs, token);
+      const long long slot = map_token(p, p.t.block_tables + (long long)s * p.t.max_blocks_per_seq, map_start[s] + token - map_cu[s], map_held[s],
+                                       map_grant[s], top);
+      if (p.slot_map) p.slot_map[token] = slot;
+    }
+  }
+}
+
 __global__ __launch_bounds__(kMapThreads) void map_kernel(TableParams p) {
+  __shared__ int cu_lds[kMapSeqs];
   const int total = p.cu_tokens[p.n_seqs];
   const long long first = ((long long)blockIdx.x * kMapThreads + threadIdx.x) * kMapTokens;
+  if ((long long)blockIdx.x * kMapThreads * kMapTokens >= total) return;
+  const int* cu = p.cu_tokens;
+  if (p.n_seqs <= kMapSeqs) {  // one round trip instead of one for each step of the search
+    for (int i = threadIdx.x; i < p.n_seqs; i += kMapThreads) cu_lds[i] = p.cu_tokens[i];
+    __syncthreads();
+    cu = cu_lds;
+  }
   if (first >= total) return;
-  int s = sequence_of(p.cu_tokens, p.n_seqs, (int)first);
-  const long long top = (long long)*p.t.free_count_out + p.cu_blocks[p.n_seqs];  // entries of the stack before the blocks were taken
-  int end = -1, start = 0, base = 0, old_held = 0;
-  long long grant = 0;
-  const int* row = nullptr;
+  int s = sequence_of(cu, p.n_seqs, (int)first);
+  const long long top = (long long)*p.t.free_count_out + p.cu_blocks[p.n_seqs];  // entries of the stack before blocks were taken
+  int end = -1, start = 0, base = 0, old_held = 0, grant = 0;
+  int* row = nullptr;
   for (int i = 0; i < kMapTokens; ++i) {
     const int token = (int)first + i;
     if (token >= total) return;
@@ -175,18 +246,11 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(TableParams p) {
       if (end <= token) continue;
       start = p.start_pos[s];
       grant = p.cu_blocks[s];
-      old_held = p.t.held_out[s] - (p.cu_blocks[s + 1] - (int)grant);
+      old_held = p.t.held_out[s] - (p.cu_blocks[s + 1] - grant);
       row = p.t.block_tables + (long long)s * p.t.max_blocks_per_seq;
     }
-    const int pos = start + (token - base), column = pos / kBlock;
-    int block;
-    if (column < old_held) {
-      block = row[column];
-    } else {
-      block = p.t.free_blocks[top - 1 - (grant + column - old_held)];
-      if (pos % kBlock == 0) const_cast<int*>(row)[column] = block;
-    }
-    if (p.slot_map) p.slot_map[token] = (long long)block * kBlock + pos % kBlock;
+    const long long slot = map_token(p, row, start + (token - base), old_held, grant, top);
+    if (p.slot_map) p.slot_map[token] = slot;
   }
 }
 
@@ -197,9 +261,12 @@ int launch_build_tables(const cronus_paged_tables* tables, const int32_t* kv_len
                         int32_t* report, void* stream) {
   const TableParams p{*tables, kv_lens, new_lens, n_seqs, cu_tokens, start_pos, cu_blocks, reinterpret_cast<long long*>(slot_map), max_tokens, report};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
+  const bool maps = n_seqs <= kPlanThreads && max_tokens <= kFewTokens;
+  const int busy = maps && max_tokens > n_seqs ? max_tokens : n_seqs;
+  const int threads = busy < kPlanThreads ? busy < 64 ? 64 : (busy + 63) / 64 * 64 : kPlanThreads;
+  hipLaunchKernelGGL(maps ? plan_kernel<true> : plan_kernel<false>, dim3(1), dim3(threads), 0, s, p);
   if (hipGetLastError() != hipSuccess) return CRONUS_ERR_HIP;
-  if (n_seqs == 0 || max_tokens == 0) return CRONUS_OK;
+  if (maps || max_tokens == 0) return CRONUS_OK;
   const unsigned per = kMapThreads * kMapTokens;
   hipLaunchKernelGGL(map_kernel, dim3(((unsigned)max_tokens + per - 1) / per), dim3(kMapThreads), 0, s, p);
   return hipGetLastError() == hipSuccess ? CRONUS_OK : CRONUS_ERR_HIP;
