@@ -8,14 +8,13 @@
 // keys, go to one XCD.  A row tile whose units lie in several shares is left as partial results (m, l, O), which
 // merge_kernel combines; a share has at most two of them, one at either end, so the workspace does not depend on the lengths.
 //
-// Eight wavefronts: WR of them side by side hold 32 rows each (a row is a drafted token and a query head of the KV head), and
-// 8 / WR such groups take every (8 / WR)-th 32-key sub-tile.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: a row is a
-// column, its lanes are l and l + 32, and P stays in registers.  K/V reach the operands in one of two ways (STAGED):
-//   streamed - few rows, bound by memory: every wave moves its own sub-tiles to LDS of its own, by DMA, so that loads in flight
-//              take no registers, and no wave waits for another;
-//   staged   - many rows, bound by products: the work-group moves tiles of kUnitKeys keys through registers (fp8 codes are
-//              converted there, once) to one of two LDS buffers, and all waves read their operands there, where each would
-//              fetch the same K/V otherwise.
+// S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: a row (a drafted token and a query head of the KV head) is a column, its
+// lanes are l and l + 32, and P stays in registers.  Two kernels, by the rows of a KV head that a sequence can have:
+//   stream_kernel - few rows, bound by memory: 8 wavefronts, WR side by side with 32 rows each, 8 / WR of which take every (8 / WR)-th
+//                   32-key sub-tile.  Each moves its own sub-tiles to LDS of its own, by DMA: loads in flight take no registers, and no
+//                   wave waits for another.
+//   tiles_kernel  - many rows, bound by products: the same waves, but tiles of kUnitKeys keys go through registers (fp8 codes are
+//                   converted there, once) to one of two LDS buffers, where all waves read their operands.
 #include <hip/hip_runtime.h>
 
 #include "cronus_internal.h"
@@ -57,7 +56,7 @@ struct Split {
 static_assert(sizeof(Split) == 32);
 
 // Floats of a slot: O, then (m in log2 units, l) of every row.
-template <int D, int WR> constexpr int kSlotFloats = 32 * WR * (D + 2);
+template <int D, int ROWS> constexpr int kSlotFloats = ROWS * (D + 2);
 
 // The sequence's lengths, or no rows where they are none that this call could serve.
 struct Lens {
@@ -70,11 +69,15 @@ __device__ __forceinline__ Lens lens_of(const TreeParams& p, int s) {
                     prefix + count <= min((long long)p.max_blocks * kBlock, kTreeMostKeys);
   return good ? Lens{prefix, (int)count, first} : Lens{0, 0, 0};
 }
-template <int WR>
+template <int ROWS>
 __device__ __forceinline__ int row_tiles(const TreeParams& p, const Lens& n) {
-  return (n.count * (p.n_q_heads / p.n_kv_heads) + 32 * WR - 1) / (32 * WR);
+  return (n.count * (p.n_q_heads / p.n_kv_heads) + ROWS - 1) / ROWS;
 }
 __device__ __forceinline__ int key_units(const Lens& n) { return (n.prefix + n.count + kUnitKeys - 1) / kUnitKeys; }
+template <int ROWS>
+__device__ __forceinline__ long long units_of(const TreeParams& p, const Lens& n) {
+  return n.count ? (long long)row_tiles<ROWS>(p, n) * key_units(n) * p.n_kv_heads : 0LL;
+}
 
 // 32 bits: which of the keys first_key .. first_key + 31 the row of drafted token `token` sees.
 __device__ __forceinline__ unsigned visible_bits(const TreeParams& p, const Lens& n, int token, int first_key) {
@@ -130,19 +133,20 @@ struct Share {
   int index, active, seq;
   bool idle;
 };
+template <int THREADS>
 struct ShareLds {
-  long long sums[kWaves], base;
+  long long sums[THREADS / 64], base;
   int seq;
 };
 
 // Thread t sums the units of sequences [t per, (t + 1) per).
-template <class Units>
-__device__ __forceinline__ Share find_share(const TreeParams& p, ShareLds& lds, const Units& units_of) {
+template <int ROWS, int THREADS>
+__device__ __forceinline__ Share find_share(const TreeParams& p, ShareLds<THREADS>& lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (p.n_seqs + kThreads - 1) / kThreads;
+  const int per = (p.n_seqs + THREADS - 1) / THREADS;
   const int s_lo = min(tid * per, p.n_seqs), s_hi = min(s_lo + per, p.n_seqs);
   long long mine = 0;
-  for (int s = s_lo; s < s_hi; ++s) mine += units_of(lens_of(p, s));
+  for (int s = s_lo; s < s_hi; ++s) mine += units_of<ROWS>(p, lens_of(p, s));
   long long incl = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -153,7 +157,7 @@ __device__ __forceinline__ Share find_share(const TreeParams& p, ShareLds& lds, 
   __syncthreads();
   Share r{};
   long long base = 0;
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < THREADS / 64; ++w) {
     if (w == wave) base = r.total;
     r.total += lds.sums[w];
   }
@@ -172,7 +176,7 @@ __device__ __forceinline__ Share find_share(const TreeParams& p, ShareLds& lds, 
   if (base <= r.begin && r.begin < base + mine) {  // one thread
     int s = s_lo;
     for (;; ++s) {
-      const long long u = units_of(lens_of(p, s));
+      const long long u = units_of<ROWS>(p, lens_of(p, s));
       if (r.begin < base + u) break;
       base += u;
     }
@@ -185,444 +189,565 @@ __device__ __forceinline__ Share find_share(const TreeParams& p, ShareLds& lds, 
   return r;
 }
 
-template <int D, bool FP8, int WR, bool STAGED>
-__global__ __launch_bounds__(512, 2) void attn_tree_kernel(TreeParams p) {
-  constexpr int NSTEP = D / 16, NDB = D / 32, ESZ = FP8 ? 1 : 2, WK = kWaves / WR, ROWS = 32 * WR;
-  constexpr int BLKB = 16 * D * ESZ;            // bytes of one (block, head) of the cache
-  constexpr int SWZ = D / 4 - 1;                // results in LDS: group x of 4 dims of row r lies at x ^ (r & SWZ)
-  constexpr int RESULT = 32 * D * 4;            // bytes of a wave's result
-  constexpr int WAVE_LDS = 2 * NSTEP * 1024 + (FP8 ? 512 : 0);  // streamed: a wave's K and V planes, or two sets of block images (fp8)
-  constexpr int TILE = kUnitKeys * D * 2 * 2;   // staged: bytes of K and V of a tile
-  static_assert(WAVE_LDS >= RESULT, "a wave's result takes the place of its planes");
-  constexpr int LDS = STAGED ? (WK > 1 && kWaves * RESULT > 2 * TILE ? kWaves * RESULT : 2 * TILE) : kWaves * WAVE_LDS;
-  __shared__ __align__(1024) unsigned char smem[LDS];
-  __shared__ float ml_lds[kWaves][32][2];
-  __shared__ ShareLds share_lds;
+// The units of one row tile in a share.
+struct Piece {
+  Lens n;
+  int seq, kv_head, unit, key_begin, key_end, kv_len, row0, n_rows;
+  long long item_end;
+  bool whole;  // all units of the row tile
+};
+struct Walk {
+  Share sh;
+  long long seq_base, at;
+  int seq;
+  Lens n;
+};
+__device__ __forceinline__ Walk begin_walk(const TreeParams& p, const Share& sh) { return Walk{sh, sh.seq_base, sh.begin, sh.seq, lens_of(p, sh.seq)}; }
+template <int ROWS>
+__device__ __forceinline__ bool next_piece(const TreeParams& p, Walk& w, Piece& it) {
+  if (w.at >= w.sh.end) return false;
+  while (w.n.count == 0 || w.at >= w.seq_base + units_of<ROWS>(p, w.n)) {  // the share has another unit, so there is another sequence
+    w.seq_base += units_of<ROWS>(p, w.n);
+    w.n = lens_of(p, ++w.seq);
+  }
+  const int n_key_units = key_units(w.n), n_tiles = row_tiles<ROWS>(p, w.n);
+  const long long rel = w.at - w.seq_base;
+  const int tile_index = (int)(rel / n_key_units);
+  it.n = w.n;
+  it.seq = w.seq;
+  it.unit = (int)(rel - (long long)tile_index * n_key_units);
+  it.kv_head = tile_index / n_tiles;
+  it.row0 = (tile_index - it.kv_head * n_tiles) * ROWS;
+  it.n_rows = min(ROWS, w.n.count * (p.n_q_heads / p.n_kv_heads) - it.row0);
+  it.item_end = w.at - it.unit + n_key_units;
+  const long long end = min(it.item_end, w.sh.end);
+  it.kv_len = w.n.prefix + w.n.count;
+  it.key_begin = it.unit * kUnitKeys;
+  it.key_end = min(it.kv_len, (it.unit + (int)(end - w.at)) * kUnitKeys);
+  it.whole = it.unit == 0 && end == it.item_end;
+  w.at = end;
+  return true;
+}
+// The tile's first piece leaves word of the others.
+__device__ __forceinline__ void note_split(const TreeParams& p, const Share& sh, const Piece& it) {
+  if (it.unit != 0 || it.whole || threadIdx.x != 0) return;
+  int last = sh.index + 1;
+  while ((last + 1) * sh.total / sh.active < it.item_end) ++last;
+  p.splits[blockIdx.x] = Split{last - sh.index + 1, sh.index, it.n_rows, it.row0, it.kv_head, it.n.first, it.n.prefix, it.n.count};
+}
 
-  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
-  const int group = p.n_q_heads / p.n_kv_heads;
-  auto units_of = [&](const Lens& n) { return n.count ? (long long)row_tiles<WR>(p, n) * key_units(n) * p.n_kv_heads : 0LL; };
-  const Share sh = find_share(p, share_lds, units_of);
-  if (tid == 0) p.splits[blockIdx.x].n_pieces = 0;
-  if (sh.idle) return;
-  int s = sh.seq;
-  long long seq_base = sh.seq_base, at = sh.begin;
-  Lens n = lens_of(p, s);
-
-  while (at < sh.end) {
-    // ---- the piece: units of one row tile
-    while (n.count == 0 || at >= seq_base + units_of(n)) {  // the share has another unit, so there is another sequence
-      seq_base += units_of(n);
-      n = lens_of(p, ++s);
-    }
-    const int n_key_units = key_units(n), n_tiles = row_tiles<WR>(p, n), kv_len = n.prefix + n.count;
-    const long long rel = at - seq_base;
-    const int tile_index = (int)(rel / n_key_units), unit = (int)(rel - (long long)tile_index * n_key_units);
-    const int kv_head = tile_index / n_tiles, tile = tile_index - kv_head * n_tiles;
-    const long long item_end = at - unit + n_key_units;
-    const long long piece_end = min(item_end, sh.end);
-    const int key_begin = unit * kUnitKeys, key_end = min(kv_len, (unit + (int)(piece_end - at)) * kUnitKeys);
-    const int row0 = tile * ROWS, n_rows = min(ROWS, n.count * group - row0);
-    const bool whole = unit == 0 && piece_end == item_end;
-
-    // ---- rows
-    const int row = min(row0 + wr * 32 + c32, n.count * group - 1);
-    const int token = row / group, head = kv_head * group + row - token * group;
-    float c = p.scale_log2e * (FP8 ? p.k_scale[kv_head] : 1.0f);
-    const unsigned flip = c < 0 ? 0x80008000u : 0u;  // the running maximum is that of the scores: a negative factor goes into q
-    c = fabsf(c);
-    if (c < 1e-37f) c = 1e-37f;  // and 0 times the -infinity of a key that is not seen is no weight
-    u32x4 qraw[NSTEP];
-    bf16x8 qreg[NSTEP];
-    const unsigned short* qp = p.q + ((long long)(n.first + token) * p.n_q_heads + head) * D + 8 * half;
-
-    f32x16 o[NDB];
-    float m = kNeg, l = 0.f;
+// 8 dims of row r of the tile, final or partial.
+template <int D>
+__device__ __forceinline__ void store_final(const TreeParams& p, const Piece& it, int r, int d, const float (&x)[8], float sum, float v_factor) {
+  const int group = p.n_q_heads / p.n_kv_heads, tok = (it.row0 + r) / group, h = it.kv_head * group + (it.row0 + r) - tok * group;
+  const float f = v_factor / sum;
+  u32x4 w;
+  if (sum == 0.f && sees_nothing(p, it.n, tok)) {
+    w = u32x4{0, 0, 0, 0};
+  } else {
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+    for (int e = 0; e < 4; ++e) w[e] = pack_bf16(x[2 * e] * f, x[2 * e + 1] * f);
+  }
+  *reinterpret_cast<u32x4*>(p.out + ((long long)(it.n.first + tok) * p.n_q_heads + h) * D + d) = w;
+}
+template <int D>
+__device__ __forceinline__ void store_partial(float* part, int r, int d, const float (&x)[8]) {
+  float* to = part + r * D + d;
+  *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
+  *reinterpret_cast<f32x4*>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+
+// What a wave keeps of 32 rows: a lane has one of them, and every second 8 of its dims.
+template <int D>
+struct Rows {
+  f32x16 o[D / 32];
+  bf16x8 q[D / 16];
+  float m, l;
+  int token;
+  __device__ __forceinline__ void clear() {
+    m = kNeg;
+    l = 0.f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  }
+  __device__ __forceinline__ void rescale(float m_new, float c) {
+    const float alpha = __builtin_amdgcn_exp2f((m - m_new) * c);
+    l *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    m = m_new;
+  }
+};
 
-    const int* table = p.block_tables + (long long)s * p.max_blocks;
-    const int last_block = (kv_len - 1) / kBlock;
-    const int pr = perm32(c32);
-
-    // ---- a sub-tile of 32 keys
-    auto scores = [&](const u32x4 (&kop)[NSTEP], f32x16& sc) {
+__device__ __forceinline__ float lane_max(const f32x16& sc) {
+  float mx = sc[0];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+  for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+  return mx;
+}
+// Keys that the row does not see.
+__device__ __forceinline__ void hide_scores(f32x16& sc, unsigned seen, int half) {
+  const unsigned own = seen >> (8 * half);
 #pragma unroll
-      for (int st = 0; st < NSTEP; ++st) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kop[st]), qreg[st], sc, 0, 0, 0);
-    };
-    auto weights = [&](f32x16& sc, int key, u32x4 (&pp)[2]) {
-      if (key + 32 > n.prefix) {
-        const unsigned own = visible_bits(p, n, token, key) >> (8 * half);
+  for (int i = 0; i < 16; ++i) sc[i] = own >> (16 * (i >> 3) + (i & 7)) & 1 ? sc[i] : -__builtin_inff();
+}
+// The V operands of a sub-tile with drafted tokens: 0 in the slots behind the last of them; true if there are infinite or NaN
+// values, in whose place is 0 then.
+template <int D>
+__device__ __forceinline__ bool tidy_values(u32x4 (&vop)[D / 16], int key, int kv_len, int half) {
+  constexpr int NSTEP = D / 16, NDB = D / 32;
+  if (key + 32 > kv_len) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[i] = own >> (16 * (i >> 3) + (i & 7)) & 1 ? sc[i] : -__builtin_inff();
-      }
-      float mx = sc[0];
+    for (int x = 0; x < NSTEP; ++x) vop[x] = zero_tail(vop[x], key + 16 * (x / NDB) + 8 * half, kv_len);
+  }
+  bool mine = false;
 #pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
-      mx = pair_max(mx);
-      // m only has to bound the scores loosely: numerators of up to 2^kLazyLog2 are as exact in bf16 as those below 1
-      if (__builtin_amdgcn_ballot_w64((mx - m) * c > kLazyLog2) != 0) {
-        const float m_new = fmaxf(m, mx);
-        const float alpha = __builtin_amdgcn_exp2f((m - m_new) * c);
-        l *= alpha;
+  for (int x = 0; x < NSTEP; ++x) mine |= not_finite(vop[x]);
+  const bool odd = __builtin_amdgcn_ballot_w64(mine) != 0;
+  if (odd) {
 #pragma unroll
-        for (int db = 0; db < NDB; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
-        m = m_new;
-      }
-      l += softmax_exp_part(sc, c, m, pp);
-    };
-    auto sums = [&](u32x4 (&vop)[NSTEP], const u32x4 (&pp)[2], int key) {
-      bool odd = false;
-      if (key + 32 > n.prefix) {
-        if (key + 32 > kv_len) {
-#pragma unroll
-          for (int x = 0; x < NSTEP; ++x) vop[x] = zero_tail(vop[x], key + 16 * (x / NDB) + 8 * half, kv_len);
-        }
-        bool mine = false;
-#pragma unroll
-        for (int x = 0; x < NSTEP; ++x) mine |= not_finite(vop[x]);
-        odd = __builtin_amdgcn_ballot_w64(mine) != 0;
-        if (odd) {
-#pragma unroll
-          for (int x = 0; x < NSTEP; ++x) vop[x] = finite_only(vop[x]);
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int db = 0; db < NDB; ++db)
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vop[t * NDB + db]), as_bf16x8(pp[t]), o[db], 0, 0, 0);
-      if (odd) {
-        // Infinite and NaN values are added to the rows that see their key, one after the other: in the product, 0 times such a value
-        // would be NaN in the others.
-        const unsigned seen = visible_bits(p, n, token, key);
+    for (int x = 0; x < NSTEP; ++x) vop[x] = finite_only(vop[x]);
+  }
+  return odd;
+}
+// Infinite and NaN values are added to the rows that see their key, one after the other: in the product, 0 times such a value would be
+// NaN in the others.
+template <int D, bool FP8>
+__device__ __forceinline__ void add_odd_values(const TreeParams& p, const Piece& it, Rows<D>& rows, const u32x4 (&pp)[2], int key, int half, int c32) {
+  constexpr int ESZ = FP8 ? 1 : 2;
+  const int* table = p.block_tables + (long long)it.seq * p.max_blocks;
+  const unsigned seen = visible_bits(p, it.n, rows.token, key);
 #pragma unroll 1
-        for (int b = 0; b < 32 && key + b < kv_len; ++b) {
-          const int x = (b >> 4) * 4 + ((b & 7) >> 1);
-          unsigned word = 0;
+  for (int b = 0; b < 32 && key + b < it.kv_len; ++b) {
+    const int x = (b >> 4) * 4 + ((b & 7) >> 1);
+    unsigned word = 0;
 #pragma unroll
-          for (int y = 0; y < 8; ++y) word = x == y ? pp[y >> 2][y & 3] : word;
-          word = __shfl(word, c32 + 32 * (b >> 3 & 1));
-          const float weight = __uint_as_float(b & 1 ? word & 0xffff0000u : word << 16);
-          const int pos = key + b;
-          const unsigned char* g =
-              p.v_pool + ((long long)table[pos / kBlock] * p.n_kv_heads + kv_head) * BLKB + (pos % kBlock / 8 * D * 8 + pos % 8) * ESZ;
+    for (int y = 0; y < 8; ++y) word = x == y ? pp[y >> 2][y & 3] : word;
+    word = __shfl(word, c32 + 32 * (b >> 3 & 1));
+    const float weight = __uint_as_float(b & 1 ? word & 0xffff0000u : word << 16);
+    const int pos = key + b;
+    const unsigned char* g = p.v_pool + ((long long)table[pos / kBlock] * p.n_kv_heads + it.kv_head) * (16 * D * ESZ) +
+                             (pos % kBlock / 8 * D * 8 + pos % 8) * ESZ;
 #pragma unroll
-          for (int db = 0; db < NDB; ++db)
+    for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int d = 32 * db + 16 * (i >> 3) + 8 * half + (i & 7);
-              float value;
-              if constexpr (FP8) value = __builtin_amdgcn_cvt_f32_fp8((int)g[d * 8], 0);
-              else value = __uint_as_float((unsigned)reinterpret_cast<const unsigned short*>(g)[d * 8] << 16);
-              const bool add = (seen >> b & 1) && (__float_as_uint(value) & 0x7f800000u) == 0x7f800000u;
-              o[db][i] = add ? __builtin_fmaf(weight, value, o[db][i]) : o[db][i];
-              asm volatile("" : "+v"(o[db][i]) : : "memory");  // one at a time: no registers for a path that is hardly ever taken
-            }
-        }
+      for (int i = 0; i < 16; ++i) {
+        const int d = 32 * db + 16 * (i >> 3) + 8 * half + (i & 7);
+        float value;
+        if constexpr (FP8) value = __builtin_amdgcn_cvt_f32_fp8((int)g[d * 8], 0);
+        else value = __uint_as_float((unsigned)reinterpret_cast<const unsigned short*>(g)[d * 8] << 16);
+        const bool add = (seen >> b & 1) && (__float_as_uint(value) & 0x7f800000u) == 0x7f800000u;
+        rows.o[db][i] = add ? __builtin_fmaf(weight, value, rows.o[db][i]) : rows.o[db][i];
+        asm volatile("" : "+v"(rows.o[db][i]) : : "memory");  // one at a time: no registers for a path that is hardly ever taken
       }
-    };
-    auto load_q = [&]() {
+  }
+}
+
+// The factor of the scores, in log2 units, and what q is multiplied with (its sign bits): the running maximum is that of the
+// scores, so a negative factor goes into q.  Not 0: 0 times the -infinity of a key that is not seen is no weight.
+template <bool FP8>
+__device__ __forceinline__ float score_factor(const TreeParams& p, int kv_head, unsigned& flip) {
+  float c = p.scale_log2e * (FP8 ? p.k_scale[kv_head] : 1.0f);
+  flip = c < 0 ? 0x80008000u : 0u;
+  c = fabsf(c);
+  return c < 1e-37f ? 1e-37f : c;
+}
+
+// Results of waves that share rows, in LDS: group x of 4 dims of row r lies at x ^ (r & mask), so that the lanes of a store and
+// of a load hit all banks.
+template <int D>
+__device__ __forceinline__ float* result_at(unsigned char* base, int r, int x) {
+  return reinterpret_cast<float*>(base) + r * D + (x ^ (r & (D / 4 - 1))) * 4;
+}
+template <int D>
+__device__ __forceinline__ void put_result(unsigned char* base, int r, const f32x16 (&o)[D / 32], int half) {
 #pragma unroll
-      for (int st = 0; st < NSTEP; ++st) qraw[st] = *reinterpret_cast<const u32x4*>(qp + 16 * st);
-    };
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      *reinterpret_cast<f32x4*>(result_at<D>(base, r, 8 * db + 4 * (h >> 1) + 2 * half + (h & 1))) =
+          f32x4{o[db][4 * h], o[db][4 * h + 1], o[db][4 * h + 2], o[db][4 * h + 3]};
+}
+// Joins the results of WK waves for 8 dims of a row and stores them.  ml: (m in log2 units, l) of every wave's rows; base: wave 0's results, `pitch`
+// bytes before those of the next.
+template <int D, int ROWS, int WK, int WAVE_ROWS>
+__device__ __forceinline__ void join_and_store(const TreeParams& p, const Piece& it, unsigned char* base, int pitch, const float (*ml)[WAVE_ROWS][2], int x,
+                                               float* part, float v_factor) {
+  const int r = x / (D / 8), d = x % (D / 8) * 8, w0 = r / WAVE_ROWS * WK, rr = r % WAVE_ROWS;
+  float top = ml[w0][rr][0], sum = 0.f;
+#pragma unroll
+  for (int w = 1; w < WK; ++w) top = fmaxf(top, ml[w0 + w][rr][0]);
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < WK; ++w) {
+    const float f = __builtin_amdgcn_exp2f(ml[w0 + w][rr][0] - top);
+    sum = __builtin_fmaf(f, ml[w0 + w][rr][1], sum);
+    const f32x4 a = *reinterpret_cast<const f32x4*>(result_at<D>(base + (w0 + w) * pitch, rr, d / 4));
+    const f32x4 b = *reinterpret_cast<const f32x4*>(result_at<D>(base + (w0 + w) * pitch, rr, d / 4 + 1));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      acc[e] = __builtin_fmaf(f, a[e], acc[e]);
+      acc[4 + e] = __builtin_fmaf(f, b[e], acc[4 + e]);
+    }
+  }
+  if (it.whole) {
+    store_final<D>(p, it, r, d, acc, sum, v_factor);
+  } else {
+    store_partial<D>(part, r, d, acc);
+    if (d == 0) {
+      part[ROWS * D + 2 * r] = top;
+      part[ROWS * D + 2 * r + 1] = sum;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ few rows
+template <int D, bool FP8, int WR>
+__global__ __launch_bounds__(kThreads, 2) void stream_kernel(TreeParams p) {
+  constexpr int NSTEP = D / 16, NDB = D / 32, ESZ = FP8 ? 1 : 2, WK = kWaves / WR, ROWS = 32 * WR;
+  constexpr int BLKB = 16 * D * ESZ;                            // bytes of one (block, head) of the cache
+  constexpr int WAVE_LDS = 2 * NSTEP * 1024 + (FP8 ? 512 : 0);  // a wave's K and V planes, or two sets of block images (fp8)
+  static_assert(WAVE_LDS >= 32 * D * 4, "a wave's result takes the place of its planes");
+  __shared__ __align__(1024) unsigned char smem[kWaves * WAVE_LDS];
+  __shared__ float ml_lds[kWaves][32][2];
+  __shared__ ShareLds<kThreads> share_lds;
+
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31, pr = perm32(c32);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
+  const int group = p.n_q_heads / p.n_kv_heads;
+  const Share sh = find_share<ROWS>(p, share_lds);
+  if (tid == 0) p.splits[blockIdx.x].n_pieces = 0;
+  if (sh.idle) return;
+  Walk walk = begin_walk(p, sh);
+  Piece it;
+  while (next_piece<ROWS>(p, walk, it)) {
+    Rows<D> rows;
+    rows.clear();
+    const int row = min(it.row0 + wr * 32 + c32, it.n.count * group - 1);
+    rows.token = row / group;
+    unsigned flip;
+    const float c = score_factor<FP8>(p, it.kv_head, flip);
+    const unsigned short* qp = p.q + ((long long)(it.n.first + rows.token) * p.n_q_heads + it.kv_head * group + row - rows.token * group) * D + 8 * half;
+    u32x4 qraw[NSTEP];
     auto pin_q = [&]() {  // waits for q here
 #pragma unroll
       for (int st = 0; st < NSTEP; ++st) {
         asm volatile("" : "+v"(qraw[st]));
-        qreg[st] = as_bf16x8(qraw[st] ^ flip);
+        rows.q[st] = as_bf16x8(qraw[st] ^ flip);
       }
     };
 
-    if constexpr (STAGED) {
-      // ---- tiles of kUnitKeys keys, one in LDS, the next in registers; piece x of a block is 16 bytes of the image in LDS
-      static_assert(WK <= kUnitKeys / 32, "a sub-tile for every group of waves");
-      constexpr int PIECES = 4 * D;                          // of K and V of a block: 8 elements each
-      constexpr int PER = kUnitKeys / kBlock * PIECES / kThreads;  // of a thread
-      using Piece = std::conditional_t<FP8, u32x2, u32x4>;
-      Piece r[PER];
-      // Table entries of 16 tiles in one register, a lane each, and of the 16 after them: an entry is there when its block is
-      // requested (loaded with each tile, they cost it their round trip).
-      constexpr int kAhead = 64 * kBlock / kUnitKeys;
-      int entries = 0, entries_next = 0;
-      auto load_table = [&](int j) { return table[min(key_begin / kBlock + j * (kUnitKeys / kBlock) + lane, last_block)]; };
-      auto fetch = [&](int j) {  // tile j of the piece
-        if (j && j % kAhead == 0) {
-          entries = entries_next;
-          entries_next = load_table(j + kAhead);
-        }
+    auto scores = [&](const u32x4 (&kop)[NSTEP], f32x16& sc) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const int x = i * kThreads + tid, b = __builtin_amdgcn_readfirstlane(x / PIECES), in = x % PIECES;
-          const long long block = __builtin_amdgcn_readlane(entries, (j % kAhead) * (kUnitKeys / kBlock) + b);
-          const unsigned char* pool = __builtin_amdgcn_readfirstlane(in / (PIECES / 2)) ? p.v_pool : p.k_pool;
-          r[i] = *reinterpret_cast<const Piece*>(pool + (block * p.n_kv_heads + kv_head) * BLKB + in % (PIECES / 2) * (8 * ESZ));
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+      for (int st = 0; st < NSTEP; ++st) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kop[st]), rows.q[st], sc, 0, 0, 0);
+    };
+    auto weights = [&](f32x16& sc, int key, u32x4 (&pp)[2]) {
+      if (key + 32 > it.n.prefix) hide_scores(sc, visible_bits(p, it.n, rows.token, key), half);
+      const float mx = pair_max(lane_max(sc));
+      // m only has to bound the scores loosely: numerators of up to 2^kLazyLog2 are as exact in bf16 as those below 1
+      if (__builtin_amdgcn_ballot_w64((mx - rows.m) * c > kLazyLog2) != 0) rows.rescale(fmaxf(rows.m, mx), c);
+      rows.l += softmax_exp_part(sc, c, rows.m, pp);
+    };
+    auto sums = [&](u32x4 (&vop)[NSTEP], const u32x4 (&pp)[2], int key) {
+      bool odd = false;
+      if (key + 32 > it.n.prefix) odd = tidy_values<D>(vop, key, it.kv_len, half);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+          rows.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vop[t * NDB + db]), as_bf16x8(pp[t]), rows.o[db], 0, 0, 0);
+      if (odd) add_odd_values<D, FP8>(p, it, rows, pp, key, half, c32);
+    };
+
+    // Sub-tiles wk, wk + WK, ... of the piece; table entries of the next 32 of them in one register, two lanes each.
+    const int* table = p.block_tables + (long long)it.seq * p.max_blocks;
+    const int last_block = (it.kv_len - 1) / kBlock;
+    int bt_reg = 0;
+    auto load_table = [&](int j0) {
+      const int u = wk + WK * (j0 + (lane >> 1));
+      bt_reg = table[min((it.key_begin + 32 * u) / kBlock + (lane & 1), last_block)];
+    };
+    auto pin_table = [&]() { asm volatile("" : "+v"(bt_reg)); };
+    const int n_sub = (it.key_end - it.key_begin + 31) / 32;
+    const int n_iter = n_sub > wk ? (n_sub - wk + WK - 1) / WK : 0;
+    lds_byte* wl = (lds_byte*)smem + wave * WAVE_LDS;
+    const unsigned wl_addr = (unsigned)(unsigned long long)wl;
+    load_table(0);
+#pragma unroll
+    for (int st = 0; st < NSTEP; ++st) qraw[st] = *reinterpret_cast<const u32x4*>(qp + 16 * st);
+    pin_table();
+    if constexpr (!FP8) {
+      const unsigned rd = wl_addr + lane * 16;  // each lane reads back the chunks that it fetched
+      const int k_off = (half * 16 + (pr & 15)) * 16, v_off = (half * D + pr) * 16;
+      auto issue_k = [&](int j) {
+        const long long b0 = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31)), b1 = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + 1);
+        const unsigned char* g = p.k_pool + (((pr >> 4) ? b1 : b0) * p.n_kv_heads + it.kv_head) * BLKB + k_off;
+#pragma unroll
+        for (int st = 0; st < NSTEP; ++st) __builtin_amdgcn_global_load_lds(g + st * 512, wl + st * 1024, 16, 0, 0);
+      };
+      auto issue_v = [&](int j) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const long long b = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + t);
+          const unsigned char* g = p.v_pool + (b * p.n_kv_heads + it.kv_head) * BLKB + v_off;
+#pragma unroll
+          for (int db = 0; db < NDB; ++db) __builtin_amdgcn_global_load_lds(g + db * 512, wl + (NSTEP + t * NDB + db) * 1024, 16, 0, 0);
         }
       };
-      auto put = [&](int buffer) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          u32x4 w;
-          if constexpr (FP8) w = fp8x8_to_bf16x8(r[i]);
-          else w = r[i];
-          *reinterpret_cast<u32x4*>(smem + buffer * TILE + (i * kThreads + tid) * 16) = w;
-        }
-      };
-      entries = load_table(0);
-      load_q();
-      if (key_end - key_begin > kAhead * kUnitKeys) entries_next = load_table(kAhead);
-      fetch(0);
-      pin_q();
-      const int n_keys_tiles = (key_end - key_begin + kUnitKeys - 1) / kUnitKeys;
-      for (int j = 0; j < n_keys_tiles; ++j) {
-        const int key0 = key_begin + j * kUnitKeys, buffer = j & 1;
-        put(buffer);
-        if (j + 1 < n_keys_tiles) fetch(j + 1);
-        __syncthreads();
-#pragma unroll
-        for (int sub = 0; sub < kUnitKeys / 32; ++sub) {
-          const int key = key0 + 32 * sub;
-          if (sub % WK != wk || key >= key_end) continue;
-          const unsigned char* tile_lds = smem + buffer * TILE + 2 * sub * (PIECES * 16);
-          u32x4 kop[NSTEP], vop[NSTEP], pp[2];
-          f32x16 sc;
-#pragma unroll
-          for (int st = 0; st < NSTEP; ++st)
-            kop[st] = *reinterpret_cast<const u32x4*>(tile_lds + (pr >> 4) * (PIECES * 16) + ((2 * st + half) * 16 + (pr & 15)) * 16);
-          scores(kop, sc);
-          weights(sc, key, pp);
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int db = 0; db < NDB; ++db)
-              vop[t * NDB + db] = *reinterpret_cast<const u32x4*>(tile_lds + t * (PIECES * 16) + PIECES * 8 + (half * D + 32 * db + pr) * 16);
-          sums(vop, pp, key);
-        }
+      if (n_iter > 0) {
+        issue_k(0);
+        issue_v(0);
       }
-      if constexpr (WK > 1) __syncthreads();  // results take the place of the tiles
-    } else {
-      // ---- sub-tiles wk, wk + WK, ... of the piece; table entries of the next 32 of them in one register, two lanes each
-      int bt_reg = 0;
-      auto load_table = [&](int j0) {
-        const int u = wk + WK * (j0 + (lane >> 1));
-        bt_reg = table[min((key_begin + 32 * u) / kBlock + (lane & 1), last_block)];
-      };
-      auto pin_table = [&]() { asm volatile("" : "+v"(bt_reg)); };
-      const int n_sub = (key_end - key_begin + 31) / 32;
-      const int n_iter = n_sub > wk ? (n_sub - wk + WK - 1) / WK : 0;
-      lds_byte* wl = (lds_byte*)smem + wave * WAVE_LDS;
-      const unsigned wl_addr = (unsigned)(unsigned long long)wl;
-      load_table(0);
-      load_q();
-      pin_table();
-      if constexpr (!FP8) {
-        const unsigned rd = wl_addr + lane * 16;  // each lane reads back the chunks that it fetched
-        const int k_off = (half * 16 + (pr & 15)) * 16, v_off = (half * D + pr) * 16;
-        auto issue_k = [&](int j) {
-          const long long b0 = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31)), b1 = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + 1);
-          const unsigned char* g = p.k_pool + (((pr >> 4) ? b1 : b0) * p.n_kv_heads + kv_head) * BLKB + k_off;
-#pragma unroll
-          for (int st = 0; st < NSTEP; ++st) __builtin_amdgcn_global_load_lds(g + st * 512, wl + st * 1024, 16, 0, 0);
-        };
-        auto issue_v = [&](int j) {
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const long long b = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + t);
-            const unsigned char* g = p.v_pool + (b * p.n_kv_heads + kv_head) * BLKB + v_off;
-#pragma unroll
-            for (int db = 0; db < NDB; ++db) __builtin_amdgcn_global_load_lds(g + db * 512, wl + (NSTEP + t * NDB + db) * 1024, 16, 0, 0);
-          }
-        };
-        if (n_iter > 0) {
-          issue_k(0);
-          issue_v(0);
-        }
-        pin_q();
-        for (int j = 0; j < n_iter; ++j) {
-          const int key = key_begin + 32 * (wk + WK * j);
-          const bool more = j + 1 < n_iter;
-          u32x4 kop[NSTEP], vop[NSTEP], pp[2];
-          f32x16 sc;
-          wait_vmcnt<NSTEP>();  // K(j) has landed; the V(j) loads behind it may still fly
-          lds_read_planes<NSTEP>(kop, rd);
-          scores(kop, sc);
-          if (more) {
-            if (((j + 1) & 31) == 0) {
-              load_table(j + 1);
-              pin_table();
-            }
-            issue_k(j + 1);
-          }
-          weights(sc, key, pp);
-          if (more) wait_vmcnt<NSTEP>();
-          else wait_vmcnt<0>();  // V(j) has landed
-          lds_read_planes<NSTEP>(vop, rd + NSTEP * 1024);
-          sums(vop, pp, key);
-          if (more) issue_v(j + 1);
-        }
-      } else {
-        // The two blocks of a sub-tile are copied whole (K: the second image 128 bytes further, so that the halves of a read hit
-        // different banks), the operands' 8-byte chunks picked out of the images and converted.  Two sets.
-        constexpr int NIB = BLKB / 1024, NIK = 2 * NIB, KSET = 2 * BLKB + 128, SET = KSET + 2 * BLKB;
-        static_assert(2 * SET <= WAVE_LDS, "two sets per wave");
-        const unsigned k_rd = wl_addr + (pr >> 4) * (BLKB + 128) + (half * 16 + (pr & 15)) * 8, v_rd = wl_addr + KSET + (half * D + pr) * 8;
-        auto issue = [&](int j) {
-          if (j && (j & 31) == 0) {
-            load_table(j);
+      pin_q();
+      for (int j = 0; j < n_iter; ++j) {
+        const int key = it.key_begin + 32 * (wk + WK * j);
+        const bool more = j + 1 < n_iter;
+        u32x4 kop[NSTEP], vop[NSTEP], pp[2];
+        f32x16 sc;
+        wait_vmcnt<NSTEP>();  // K(j) has landed; the V(j) loads behind it may still fly
+        lds_read_planes<NSTEP>(kop, rd);
+        scores(kop, sc);
+        if (more) {
+          if (((j + 1) & 31) == 0) {
+            load_table(j + 1);
             pin_table();
           }
-          lds_byte* set = wl + (j & 1) * SET;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {  // K of both blocks, then V
-            const long long b = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + (x & 1));
-            const unsigned char* g = (x < 2 ? p.k_pool : p.v_pool) + (b * p.n_kv_heads + kv_head) * BLKB + lane * 16;
-#pragma unroll
-            for (int i = 0; i < NIB; ++i)
-              __builtin_amdgcn_global_load_lds(g + i * 1024, set + (x < 2 ? x * (BLKB + 128) : KSET + (x - 2) * BLKB) + i * 1024, 16, 0, 0);
-          }
-        };
-        if (n_iter > 0) issue(0);
-        if (n_iter > 1) issue(1);
-        pin_q();
-        for (int j = 0; j < n_iter; ++j) {
-          const int key = key_begin + 32 * (wk + WK * j);
-          const bool more = j + 1 < n_iter;  // sub-tile j + 1 has been requested
-          u32x4 kop[NSTEP], vop[NSTEP], pp[2];
-          u32x2 codes[NSTEP];
-          f32x16 sc;
-          if (more) wait_vmcnt<3 * NIK>();
-          else wait_vmcnt<NIK>();  // K(j) has landed
-          if constexpr (NSTEP == 8) lds_read8_b64<0, 256, 512, 768, 1024, 1280, 1536, 1792>(codes, k_rd + (j & 1) * SET);
-          else lds_read4_b64<0, 256, 512, 768>(codes, k_rd + (j & 1) * SET);
-#pragma unroll
-          for (int x = 0; x < NSTEP; ++x) kop[x] = fp8x8_to_bf16x8(codes[x]);
-          scores(kop, sc);
-          weights(sc, key, pp);
-          if (more) wait_vmcnt<2 * NIK>();
-          else wait_vmcnt<0>();  // V(j) has landed
-          if constexpr (NSTEP == 8) lds_read8_b64<0, 256, 512, 768, BLKB, BLKB + 256, BLKB + 512, BLKB + 768>(codes, v_rd + (j & 1) * SET);
-          else lds_read4_b64<0, 256, BLKB, BLKB + 256>(codes, v_rd + (j & 1) * SET);
-          if (j + 2 < n_iter) issue(j + 2);  // the set is free again
-#pragma unroll
-          for (int x = 0; x < NSTEP; ++x) vop[x] = fp8x8_to_bf16x8(codes[x]);
-          sums(vop, pp, key);
+          issue_k(j + 1);
         }
+        weights(sc, key, pp);
+        if (more) wait_vmcnt<NSTEP>();
+        else wait_vmcnt<0>();  // V(j) has landed
+        lds_read_planes<NSTEP>(vop, rd + NSTEP * 1024);
+        sums(vop, pp, key);
+        if (more) issue_v(j + 1);
+      }
+    } else {
+      // The two blocks of a sub-tile are copied whole (K: the second image 128 bytes further, so that the halves of a read hit
+      // different banks), the operands' 8-byte chunks picked out of the images and converted.  Two sets.
+      constexpr int NIB = BLKB / 1024, NIK = 2 * NIB, KSET = 2 * BLKB + 128, SET = KSET + 2 * BLKB;
+      static_assert(2 * SET <= WAVE_LDS, "two sets per wave");
+      const unsigned k_rd = wl_addr + (pr >> 4) * (BLKB + 128) + (half * 16 + (pr & 15)) * 8, v_rd = wl_addr + KSET + (half * D + pr) * 8;
+      auto issue = [&](int j) {
+        if (j && (j & 31) == 0) {
+          load_table(j);
+          pin_table();
+        }
+        lds_byte* set = wl + (j & 1) * SET;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {  // K of both blocks, then V
+          const long long b = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + (x & 1));
+          const unsigned char* g = (x < 2 ? p.k_pool : p.v_pool) + (b * p.n_kv_heads + it.kv_head) * BLKB + lane * 16;
+#pragma unroll
+          for (int i = 0; i < NIB; ++i)
+            __builtin_amdgcn_global_load_lds(g + i * 1024, set + (x < 2 ? x * (BLKB + 128) : KSET + (x - 2) * BLKB) + i * 1024, 16, 0, 0);
+        }
+      };
+      if (n_iter > 0) issue(0);
+      if (n_iter > 1) issue(1);
+      pin_q();
+      for (int j = 0; j < n_iter; ++j) {
+        const int key = it.key_begin + 32 * (wk + WK * j);
+        const bool more = j + 1 < n_iter;  // sub-tile j + 1 has been requested
+        u32x4 kop[NSTEP], vop[NSTEP], pp[2];
+        u32x2 codes[NSTEP];
+        f32x16 sc;
+        if (more) wait_vmcnt<3 * NIK>();
+        else wait_vmcnt<NIK>();  // K(j) has landed
+        if constexpr (NSTEP == 8) lds_read8_b64<0, 256, 512, 768, 1024, 1280, 1536, 1792>(codes, k_rd + (j & 1) * SET);
+        else lds_read4_b64<0, 256, 512, 768>(codes, k_rd + (j & 1) * SET);
+#pragma unroll
+        for (int x = 0; x < NSTEP; ++x) kop[x] = fp8x8_to_bf16x8(codes[x]);
+        scores(kop, sc);
+        weights(sc, key, pp);
+        if (more) wait_vmcnt<2 * NIK>();
+        else wait_vmcnt<0>();  // V(j) has landed
+        if constexpr (NSTEP == 8) lds_read8_b64<0, 256, 512, 768, BLKB, BLKB + 256, BLKB + 512, BLKB + 768>(codes, v_rd + (j & 1) * SET);
+        else lds_read4_b64<0, 256, BLKB, BLKB + 256>(codes, v_rd + (j & 1) * SET);
+        if (j + 2 < n_iter) issue(j + 2);  // the set is free again
+#pragma unroll
+        for (int x = 0; x < NSTEP; ++x) vop[x] = fp8x8_to_bf16x8(codes[x]);
+        sums(vop, pp, key);
       }
     }
-    l = pair_sum(l);
 
-    // ---- results: final rows, or a slot of the partial results
-    float* part = p.partials + (long long)(2 * sh.index + (unit == 0 ? 1 : 0)) * kSlotFloats<D, WR>;
-    const float v_factor = FP8 ? p.v_scale[kv_head] : 1.0f;
-    auto store_final = [&](int r, int d, const float (&x)[8], float sum) {  // 8 dims of row r of the tile
-      const int tok = (row0 + r) / group, h = kv_head * group + (row0 + r) - tok * group;
-      const float f = v_factor / sum;
-      u32x4 w;
-      if (sum == 0.f && sees_nothing(p, n, tok)) {
-        w = u32x4{0, 0, 0, 0};
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = pack_bf16(x[2 * e] * f, x[2 * e + 1] * f);
+    put_result<D>(smem + wave * WAVE_LDS, c32, rows.o, half);
+    rows.l = pair_sum(rows.l);
+    if (half == 0) {
+      ml_lds[wave][c32][0] = rows.m * c;
+      ml_lds[wave][c32][1] = rows.l;
+    }
+    __syncthreads();
+    float* part = p.partials + (long long)(2 * sh.index + (it.unit == 0 ? 1 : 0)) * kSlotFloats<D, ROWS>;
+    const float v_factor = FP8 ? p.v_scale[it.kv_head] : 1.0f;
+    for (int x = tid; x < it.n_rows * (D / 8); x += kThreads) join_and_store<D, ROWS, WK, 32>(p, it, smem, WAVE_LDS, ml_lds, x, part, v_factor);
+    __syncthreads();
+    note_split(p, sh, it);
+  }
+}
+
+// ----------------------------------------------------------------------------------------------------------- many rows
+template <int D, bool FP8, int WR>
+__global__ __launch_bounds__(kThreads, 2) void tiles_kernel(TreeParams p) {
+  constexpr int NSTEP = D / 16, NDB = D / 32, ESZ = FP8 ? 1 : 2, WK = kWaves / WR, ROWS = 32 * WR;
+  constexpr int BLKB = 16 * D * ESZ;
+  constexpr int PIECES = 4 * D;                           // of K and V of a block: 8 elements each, 16 bytes in LDS
+  constexpr int TILE = kUnitKeys / kBlock * PIECES * 16;  // bytes of a tile
+  constexpr int PER = TILE / 16 / kThreads;               // pieces of a thread
+  constexpr int kTiles = 2, SUBS = kUnitKeys / 32 / WK;   // tiles in LDS; a wave's sub-tiles of one: wk, wk + WK, ...
+  static_assert(SUBS >= 1, "a sub-tile for every wave");
+  constexpr int RESULT = 32 * D * 4;
+  constexpr int LDS = WK > 1 && kWaves * RESULT > kTiles * TILE ? kWaves * RESULT : kTiles * TILE;
+  using Codes = std::conditional_t<FP8, u32x2, u32x4>;
+  __shared__ __align__(1024) unsigned char smem[LDS];
+  __shared__ float ml_lds[WK > 1 ? kWaves : 1][32][2];
+  __shared__ ShareLds<kThreads> share_lds;
+
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31, pr = perm32(c32);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
+  const int group = p.n_q_heads / p.n_kv_heads;
+  const Share sh = find_share<ROWS>(p, share_lds);
+  if (tid == 0) p.splits[blockIdx.x].n_pieces = 0;
+  if (sh.idle) return;
+  Walk walk = begin_walk(p, sh);
+  Piece it;
+  while (next_piece<ROWS>(p, walk, it)) {
+    Rows<D> rows;
+    rows.clear();
+    const int row = min(it.row0 + wr * 32 + c32, it.n.count * group - 1);
+    rows.token = row / group;
+    unsigned flip;
+    const float c = score_factor<FP8>(p, it.kv_head, flip);
+    const int* table = p.block_tables + (long long)it.seq * p.max_blocks;
+    const int last_block = (it.kv_len - 1) / kBlock;
+    const int n_tiles = (it.key_end - it.key_begin + kUnitKeys - 1) / kUnitKeys;
+
+    // Table entries of 16 tiles in one register, a lane each, and of the 16 after them: an entry is there when its block is
+    // requested (loaded with each tile, they cost it their round trip).
+    constexpr int kAhead = 64 * kBlock / kUnitKeys;
+    auto load_table = [&](int j) { return table[min(it.key_begin / kBlock + j * (kUnitKeys / kBlock) + lane, last_block)]; };
+    int entries = load_table(0), entries_next = 0;
+    if (n_tiles > kAhead) entries_next = load_table(kAhead);
+    Codes r[PER];
+    auto fetch = [&](int j) {  // tile j of the piece
+      if (j && j % kAhead == 0) {
+        entries = entries_next;
+        entries_next = load_table(j + kAhead);
       }
-      *reinterpret_cast<u32x4*>(p.out + ((long long)(n.first + tok) * p.n_q_heads + h) * D + d) = w;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int x = i * kThreads + tid, b = __builtin_amdgcn_readfirstlane(x / PIECES), in = x % PIECES;
+        const long long block = __builtin_amdgcn_readlane(entries, (j % kAhead) * (kUnitKeys / kBlock) + b);
+        const unsigned char* pool = __builtin_amdgcn_readfirstlane(in / (PIECES / 2)) ? p.v_pool : p.k_pool;
+        r[i] = *reinterpret_cast<const Codes*>(pool + (block * p.n_kv_heads + it.kv_head) * BLKB + in % (PIECES / 2) * (8 * ESZ));
+      }
     };
-    auto store_partial = [&](int r, int d, const float (&x)[8]) {
-      float* to = part + r * D + d;
-      *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
-      *reinterpret_cast<f32x4*>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
+    auto put = [&](int buffer) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        u32x4 w;
+        if constexpr (FP8) w = fp8x8_to_bf16x8(r[i]);
+        else w = r[i];
+        *reinterpret_cast<u32x4*>(smem + buffer * TILE + (i * kThreads + tid) * 16) = w;
+      }
     };
+    fetch(0);
+    {
+      const unsigned short* qp =
+          p.q + ((long long)(it.n.first + rows.token) * p.n_q_heads + it.kv_head * group + row - rows.token * group) * D + 8 * half;
+#pragma unroll
+      for (int st = 0; st < NSTEP; ++st) rows.q[st] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + 16 * st) ^ flip);
+    }
+    // One barrier a tile: a wave that puts tile j + 1 has passed the barrier of tile j, so every wave has left tile j - 1, whose place it takes.
+    for (int j = 0; j < n_tiles; ++j) {
+      const unsigned char* buffer = smem + (j & 1) * TILE;
+      put(j & 1);
+      if (j + 1 < n_tiles) fetch(j + 1);
+      __syncthreads();
+#pragma unroll
+      for (int x = 0; x < SUBS; ++x) {
+        const int key = it.key_begin + j * kUnitKeys + 32 * (wk + WK * x);
+        if (key >= it.key_end) break;
+        const unsigned char* lds = buffer + 2 * (wk + WK * x) * (PIECES * 16);
+        u32x4 kop[NSTEP], vop[NSTEP], pp[2];
+        f32x16 sc;
+#pragma unroll
+        for (int st = 0; st < NSTEP; ++st)
+          kop[st] = *reinterpret_cast<const u32x4*>(lds + (pr >> 4) * (PIECES * 16) + ((2 * st + half) * 16 + (pr & 15)) * 16);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+        for (int st = 0; st < NSTEP; ++st) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kop[st]), rows.q[st], sc, 0, 0, 0);
+        const bool tail = key + 32 > it.n.prefix;
+        if (tail) hide_scores(sc, visible_bits(p, it.n, rows.token, key), half);
+        const float mx = pair_max(lane_max(sc));
+        if (__builtin_amdgcn_ballot_w64((mx - rows.m) * c > kLazyLog2) != 0) rows.rescale(fmaxf(rows.m, mx), c);  // as in stream_kernel
+        rows.l += softmax_exp_part(sc, c, rows.m, pp);
+#pragma unroll
+        for (int y = 0; y < NSTEP; ++y)
+          vop[y] = *reinterpret_cast<const u32x4*>(lds + y / NDB * (PIECES * 16) + PIECES * 8 + (half * D + y % NDB * 32 + pr) * 16);
+        bool odd = false;
+        if (tail) odd = tidy_values<D>(vop, key, it.kv_len, half);
+#pragma unroll
+        for (int y = 0; y < NSTEP; ++y)
+          rows.o[y % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vop[y]), as_bf16x8(pp[y / NDB]), rows.o[y % NDB], 0, 0, 0);
+        if (odd) add_odd_values<D, FP8>(p, it, rows, pp, key, half, c32);
+      }
+    }
+
+    float* part = p.partials + (long long)(2 * sh.index + (it.unit == 0 ? 1 : 0)) * kSlotFloats<D, ROWS>;
+    const float v_factor = FP8 ? p.v_scale[it.kv_head] : 1.0f;
+    __syncthreads();  // LDS is no longer read: the next piece's tiles, or the results, take the place of these
+    rows.l = pair_sum(rows.l);
     if constexpr (WK == 1) {
-      const int r = wr * 32 + c32;
-      if (r < n_rows) {
+      const int r0 = wr * 32 + c32;
+      if (r0 < it.n_rows) {
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = o[db][8 * h + e];
+            for (int e = 0; e < 8; ++e) x[e] = rows.o[db][8 * h + e];
             const int d = 32 * db + 16 * h + 8 * half;
-            if (whole) store_final(r, d, x, l);
-            else store_partial(r, d, x);
+            if (it.whole) store_final<D>(p, it, r0, d, x, rows.l, v_factor);
+            else store_partial<D>(part, r0, d, x);
           }
-        if (!whole && half == 0) {
-          part[ROWS * D + 2 * r] = m * c;
-          part[ROWS * D + 2 * r + 1] = l;
+        if (!it.whole && half == 0) {
+          part[ROWS * D + 2 * r0] = rows.m * c;
+          part[ROWS * D + 2 * r0 + 1] = rows.l;
         }
       }
-      __syncthreads();  // before the next piece's first tile: LDS is still being read
     } else {
-      constexpr int PITCH = STAGED ? RESULT : WAVE_LDS;
-      float* mine = reinterpret_cast<float*>(smem + wave * PITCH) + c32 * D;
-#pragma unroll
-      for (int db = 0; db < NDB; ++db)
-#pragma unroll
-        for (int h = 0; h < 4; ++h)
-          *reinterpret_cast<f32x4*>(mine + ((8 * db + 4 * (h >> 1) + 2 * half + (h & 1)) ^ (c32 & SWZ)) * 4) =
-              f32x4{o[db][4 * h], o[db][4 * h + 1], o[db][4 * h + 2], o[db][4 * h + 3]};
+      put_result<D>(smem + wave * RESULT, c32, rows.o, half);
       if (half == 0) {
-        ml_lds[wave][c32][0] = m * c;
-        ml_lds[wave][c32][1] = l;
+        ml_lds[wave][c32][0] = rows.m * c;
+        ml_lds[wave][c32][1] = rows.l;
       }
       __syncthreads();
-      for (int x = tid; x < n_rows * (D / 8); x += kThreads) {
-        const int r = x / (D / 8), d = x % (D / 8) * 8, w0 = r / 32 * WK, rr = r % 32;
-        float top = ml_lds[w0][rr][0], sum = 0.f;
-#pragma unroll
-        for (int w = 1; w < WK; ++w) top = fmaxf(top, ml_lds[w0 + w][rr][0]);
-        float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < WK; ++w) {
-          const float f = __builtin_amdgcn_exp2f(ml_lds[w0 + w][rr][0] - top);
-          sum = __builtin_fmaf(f, ml_lds[w0 + w][rr][1], sum);
-          const float* from = reinterpret_cast<const float*>(smem + (w0 + w) * PITCH) + rr * D;
-          const f32x4 a = *reinterpret_cast<const f32x4*>(from + ((d / 4) ^ (rr & SWZ)) * 4);
-          const f32x4 b = *reinterpret_cast<const f32x4*>(from + ((d / 4 + 1) ^ (rr & SWZ)) * 4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            acc[e] = __builtin_fmaf(f, a[e], acc[e]);
-            acc[4 + e] = __builtin_fmaf(f, b[e], acc[4 + e]);
-          }
-        }
-        if (whole) {
-          store_final(r, d, acc, sum);
-        } else {
-          store_partial(r, d, acc);
-          if (d == 0) {
-            part[ROWS * D + 2 * r] = top;
-            part[ROWS * D + 2 * r + 1] = sum;
-          }
-        }
-      }
+      for (int x = tid; x < it.n_rows * (D / 8); x += kThreads) join_and_store<D, ROWS, WK, 32>(p, it, smem, RESULT, ml_lds, x, part, v_factor);
       __syncthreads();
     }
-    if (unit == 0 && !whole && tid == 0) {
-      int last = sh.index + 1;
-      while ((last + 1) * sh.total / sh.active < item_end) ++last;
-      p.splits[blockIdx.x] = Split{last - sh.index + 1, sh.index, n_rows, row0, kv_head, n.first, n.prefix, n.count};
-    }
-    at = piece_end;
+    note_split(p, sh, it);
   }
 }
 
 // Combines the pieces of the row tile that work-group blockIdx.x began and others went on with; a thread has 4 dims of a row.
-template <int D, bool FP8, int WR>
+template <int D, bool FP8, int ROWS>
 __global__ __launch_bounds__(256) void merge_kernel(TreeParams p) {
-  constexpr int kRows = 1024 / D, ROWS = 32 * WR;
+  constexpr int kRows = 1024 / D;
   const Split sp = p.splits[blockIdx.x];
   const int r = blockIdx.y * kRows + (int)threadIdx.x / (D / 4), d = (int)threadIdx.x % (D / 4) * 4;
   if (r >= (sp.n_pieces ? sp.n_rows : 0)) return;
   float top = kNeg, sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   for (int i = 0; i < sp.n_pieces; ++i) {
-    const float* part = p.partials + (long long)(2 * (sp.share + i) + (i == 0)) * kSlotFloats<D, WR>;
+    const float* part = p.partials + (long long)(2 * (sp.share + i) + (i == 0)) * kSlotFloats<D, ROWS>;
     const float m = part[ROWS * D + 2 * r], l = part[ROWS * D + 2 * r + 1];
     const f32x4 o = *reinterpret_cast<const f32x4*>(part + r * D + d);
     const float m_new = fmaxf(top, m);
@@ -639,35 +764,36 @@ __global__ __launch_bounds__(256) void merge_kernel(TreeParams p) {
   *reinterpret_cast<u32x2*>(p.out + ((long long)(sp.first_token + token) * p.n_q_heads + head) * D + d) = w;
 }
 
-// Wavefronts side by side: as many as it takes for a sequence's rows of a KV head, up to all.
-int waves_of_rows(const cronus_kv_cache* cache, int32_t max_rows) {
+// Rows of a tile: as many as it takes for a sequence's rows of a KV head, up to 256.
+int rows_of_tile(const cronus_kv_cache* cache, int32_t max_rows) {
   const long long rows = (long long)max_rows * (cache->num_q_heads / cache->num_kv_heads);
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+  return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
 }
 
 size_t split_bytes(int n_cus) { return ((size_t)n_cus * sizeof(Split) + 255) / 256 * 256; }
 
-template <int D, bool FP8, int WR>
+template <int D, bool FP8, int ROWS>
 int launch(const TreeParams& p, int n_cus, hipStream_t stream) {
-  hipLaunchKernelGGL((attn_tree_kernel<D, FP8, WR, (WR >= 4)>), dim3(n_cus), dim3(kThreads), 0, stream, p);
+  if constexpr (ROWS <= 64) hipLaunchKernelGGL((stream_kernel<D, FP8, ROWS / 32>), dim3(n_cus), dim3(kThreads), 0, stream, p);
+  else hipLaunchKernelGGL((tiles_kernel<D, FP8, ROWS / 32>), dim3(n_cus), dim3(kThreads), 0, stream, p);
   if (hipGetLastError() != hipSuccess) return CRONUS_ERR_HIP;
-  hipLaunchKernelGGL((merge_kernel<D, FP8, WR>), dim3(n_cus, 32 * WR * D / 1024), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL((merge_kernel<D, FP8, ROWS>), dim3(n_cus, ROWS * D / 1024), dim3(256), 0, stream, p);
   return hipGetLastError() == hipSuccess ? CRONUS_OK : CRONUS_ERR_HIP;
 }
 template <int D, bool FP8>
-int launch_rows(const TreeParams& p, int waves, int n_cus, hipStream_t stream) {
-  switch (waves) {
-    case 1: return launch<D, FP8, 1>(p, n_cus, stream);
-    case 2: return launch<D, FP8, 2>(p, n_cus, stream);
-    case 4: return launch<D, FP8, 4>(p, n_cus, stream);
-    default: return launch<D, FP8, 8>(p, n_cus, stream);
+int launch_rows(const TreeParams& p, int rows, int n_cus, hipStream_t stream) {
+  switch (rows) {
+    case 32: return launch<D, FP8, 32>(p, n_cus, stream);
+    case 64: return launch<D, FP8, 64>(p, n_cus, stream);
+    case 128: return launch<D, FP8, 128>(p, n_cus, stream);
+    default: return launch<D, FP8, 256>(p, n_cus, stream);
   }
 }
 
 }  // namespace
 
 size_t attn_tree_workspace(const cronus_kv_cache* cache, int32_t max_rows, int n_cus) {
-  const size_t slot = (size_t)32 * waves_of_rows(cache, max_rows) * (cache->head_dim + 2) * sizeof(float);
+  const size_t slot = (size_t)rows_of_tile(cache, max_rows) * (cache->head_dim + 2) * sizeof(float);
   return split_bytes(n_cus) + (2 * slot * n_cus + 255) / 256 * 256;
 }
 
@@ -694,11 +820,11 @@ int launch_attn_tree(const cronus_kv_cache* cache, const void* q, void* out, con
   p.scale_log2e = sm_scale * 1.4426950408889634f;
   p.splits = static_cast<Split*>(workspace);
   p.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + split_bytes(n_cus));
-  const int waves = waves_of_rows(cache, max_rows);
+  const int rows = rows_of_tile(cache, max_rows);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool fp8 = cache->kv_dtype == CRONUS_KV_FP8_E4M3;
-  if (cache->head_dim == 128) return fp8 ? launch_rows<128, true>(p, waves, n_cus, s) : launch_rows<128, false>(p, waves, n_cus, s);
-  return fp8 ? launch_rows<64, true>(p, waves, n_cus, s) : launch_rows<64, false>(p, waves, n_cus, s);
+  if (cache->head_dim == 128) return fp8 ? launch_rows<128, true>(p, rows, n_cus, s) : launch_rows<128, false>(p, rows, n_cus, s);
+  return fp8 ? launch_rows<64, true>(p, rows, n_cus, s) : launch_rows<64, false>(p, rows, n_cus, s);
 }
 
 }  // namespace cronus
