@@ -347,7 +347,7 @@ int cronus_build_tables(const cronus_paged_tables* tables, const int32_t* kv_len
  * A sequence with n <= 0 or n > max_rows, a negative prefix or more than 16 * max_blocks_per_seq (or 2^31 - 256) positions is
  * passed over: its rows of out are left as they were, as are rows outside of all sequences.
  * The results of a call depend on its arguments alone (no atomics), and on the number of CUs.
- * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.
+ * Errors: INVALID_ARG (also: n_seqs * Hkv * ceil(max_rows * Hq / Hkv / 256) of 2^31 / CUs and more), UNSUPPORTED, WORKSPACE, HIP.
  */
 int cronus_attn_tree(const cronus_kv_cache* cache, const void* q, void* out, const int32_t* prefix_lens, const int32_t* cu_rows,
                      const uint64_t* mask, int32_t mask_words, const int32_t* block_tables, int32_t max_blocks_per_seq,

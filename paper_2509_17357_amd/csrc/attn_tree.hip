@@ -3,7 +3,7 @@
 //     out_i = sum_j w_ij V_j / sum_j w_ij,  w_ij = exp(scale <q_i, K_j> - m_i),  j < L or (j = L + k, k < n, bit k of mask_i).
 //
 // The host does not know the lengths, so a launch has as many work-groups as the GPU has CUs, and each finds its share itself: the
-// batch is a sequence of U units (a row tile of a KV head against kUnitKeys keys; keys run fastest, then row tiles, heads, sequences),
+// batch is a sequence of U units (a row tile of a KV head against unit_keys keys; keys run fastest, then row tiles, heads, sequences),
 // and share l of A = min(work-groups, U) is units [l U / A, (l + 1) U / A), at least one.  Neighbouring shares, whose row tiles read the same
 // keys, go to one XCD.  A row tile whose units lie in several shares is left as partial results (m, l, O), which
 // merge_kernel combines; a share has at most two of them, one at either end, so the workspace does not depend on the lengths.
@@ -13,9 +13,10 @@
 //   stream_kernel - few rows, bound by memory: 8 wavefronts, WR side by side with 32 rows each, 8 / WR of which take every (8 / WR)-th
 //                   32-key sub-tile.  Each moves its own sub-tiles to LDS of its own, by DMA: loads in flight take no registers, and no
 //                   wave waits for another.
-//   tiles_kernel  - many rows, bound by products: the same waves, but tiles of kUnitKeys keys go through registers (fp8 codes are
+//   tiles_kernel  - many rows, bound by products: the same waves, but tiles of kTileKeys keys go through registers (fp8 codes are
 //                   converted there, once) to one of two LDS buffers, where all waves read their operands.
 #include <hip/hip_runtime.h>
+#include <algorithm>
 
 #include "cronus_internal.h"
 #include "lane_ops.h"
@@ -23,7 +24,28 @@
 namespace cronus {
 namespace {
 
-constexpr int kUnitKeys = 64;
+// Rows of a tile.  A batch of at most kFewRowTiles tiles of 32 rows is streamed, however many rows a sequence has: the tiles of a sequence read
+// the same K/V at the same time on one XCD, and there are CUs for them all.  us a pass, 32 / 128 rows: 100 rows (fp8, 3 sequences of about 700) 14.5 / 26.3,
+// 126 rows (7 of 119 .. 1278) 15.8 / 28.0, 252 (one of 5000) 23.4 / 34.0; beyond it, 132 rows (fp8, 13 of 56 .. 3028) 65.7 / 45.6, 301 (9 of 106 .. 10230)
+// 65.5 / 52.5, 116 (21 of 104 .. 389) 34.6 / 27.3.  256 rows read K/V half as often but have half the work-groups: from 192 rows and kManyRowTiles on.  128 / 256 rows: 256
+// rows (32 of 1000 .. 8000) 254 / 205, 488 (fp8, 16 of 8000 .. 32000) 864 / 723; 301 as above 52.5 / 58.5, 184 (50 of 82 .. 2258, D = 64) 29.8 / 31.5.
+constexpr long long kFewRowTiles = 352, kManyRowTiles = 1536;
+// A cut between two shares that is one unit from an end of an item moves there: a piece costs a work-group about 5 us before its first
+// product and behind its last one, and a row tile cut in two is written and read once more.  us a pass with 0 / 1 / 2 units: a sequence of 3300
+// keys and 21 tokens, 7 heads a KV head, 24.2 / 21.7 / 22.2; fp8, 13 of 56 .. 3028 and 4 .. 33 46.3 / 41.2 / 41.0; 9 of 106 .. 10230 66.8 / 60.6 / 60.5; 25 chains
+// of 500 .. 4097 35.5 / 36.0 / 39.2 (and with 3, 32 trees of 64 213 instead of 204).
+constexpr int kSnapUnits = 1;
+// Where the tables have room for so many steps of a work-group at most (1792 keys streamed, 448 in tiles), a unit holds all keys of a
+// sequence: no row tile is split, so there is no merge launch, and every work-group has whole items.  us a pass, cut / whole: a tree of 8 behind
+// 256 keys 12.5 / 9.5; 31 single tokens behind 40 .. 346 19.2 / 11.6; 11 trees of 5 .. 28, fp8, behind 17 .. 700 19.8 / 13.1; 166 single tokens behind
+// 52 .. 1162 106.6 / 94.9.  With 12 steps 8 trees of 12 .. 32 behind 200 .. 3000 take 27.9 instead of 30.2, but 146 single tokens behind
+// 398 .. 3011, 7 heads a KV head, 112.7 instead of 90.2.
+constexpr int kWholeSteps = 7;
+constexpr int kNonTemporal = 2;  // cache policy operand of a transfer: the instruction's nt bit
+constexpr int kTileKeys = 64;             // of a tile in LDS (tiles_kernel)
+// Units times work-groups stay below this, for any lengths that the tables have room for: shares are computed in 32 bits, where a 64-bit
+// division is 140 instructions.
+constexpr long long kMostUnitShares = 1LL << 31;
 
 struct TreeParams {
   const unsigned short* q;
@@ -39,6 +61,8 @@ struct TreeParams {
   float* partials;        // two slots a work-group
   struct Split* splits;   // one a work-group
   int mask_words, max_blocks, n_seqs, max_rows, n_q_heads, n_kv_heads;
+  int unit_keys;  // a multiple of what a work-group takes in one step
+  bool whole;     // a unit holds all keys of any sequence
   float scale_log2e;
 };
 
@@ -73,10 +97,10 @@ template <int ROWS>
 __device__ __forceinline__ int row_tiles(const TreeParams& p, const Lens& n) {
   return (n.count * (p.n_q_heads / p.n_kv_heads) + ROWS - 1) / ROWS;
 }
-__device__ __forceinline__ int key_units(const Lens& n) { return (n.prefix + n.count + kUnitKeys - 1) / kUnitKeys; }
+__device__ __forceinline__ int key_units(const TreeParams& p, const Lens& n) { return (int)((unsigned)(n.prefix + n.count + p.unit_keys - 1) / (unsigned)p.unit_keys); }
 template <int ROWS>
-__device__ __forceinline__ long long units_of(const TreeParams& p, const Lens& n) {
-  return n.count ? (long long)row_tiles<ROWS>(p, n) * key_units(n) * p.n_kv_heads : 0LL;
+__device__ __forceinline__ int units_of(const TreeParams& p, const Lens& n) {
+  return n.count ? row_tiles<ROWS>(p, n) * key_units(p, n) * p.n_kv_heads : 0;
 }
 
 // 32 bits: which of the keys first_key .. first_key + 31 the row of drafted token `token` sees.
@@ -129,63 +153,85 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 v) {
 
 // A work-group's share of the batch, and the sequence that it begins in.
 struct Share {
-  long long begin, end, total, seq_base;  // units; seq_base: those before sequence seq
+  int begin, end, total, seq_base;  // units; seq_base: those before sequence seq
   int index, active, seq;
-  bool idle;
+  Lens n;  // of that sequence
 };
-template <int THREADS>
 struct ShareLds {
-  long long sums[THREADS / 64], base;
-  int seq;
+  int sums[kWaves], base[2], seq[2];
+  Lens n[2];
 };
+__device__ __forceinline__ int cut(int index, int total, int active) { return (int)((unsigned)index * (unsigned)total / (unsigned)active); }
+// A cut at `at` in an item of `units` units from `first` on, moved to an end of the item that is near.
+__device__ __forceinline__ int snap(int at, int first, int units) {
+  return at - first <= kSnapUnits ? first : first + units - at <= kSnapUnits ? first + units : at;
+}
 
-// Thread t sums the units of sequences [t per, (t + 1) per).
-template <int ROWS, int THREADS>
-__device__ __forceinline__ Share find_share(const TreeParams& p, ShareLds<THREADS>& lds) {
+// Thread t sums the units of sequences [t per, (t + 1) per).  The share is empty (begin >= end) where there is nothing to do.
+template <int ROWS>
+__device__ __forceinline__ Share find_share(const TreeParams& p, ShareLds& lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (p.n_seqs + THREADS - 1) / THREADS;
+  const int per = (p.n_seqs + kThreads - 1) / kThreads;
   const int s_lo = min(tid * per, p.n_seqs), s_hi = min(s_lo + per, p.n_seqs);
-  long long mine = 0;
-  for (int s = s_lo; s < s_hi; ++s) mine += units_of<ROWS>(p, lens_of(p, s));
-  long long incl = mine;
+  int mine = 0;
+  Lens n{};
+  for (int s = s_lo; s < s_hi; ++s) {
+    n = lens_of(p, s);
+    mine += units_of<ROWS>(p, n);
+  }
+  int incl = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const long long y = __shfl(incl, lane - d < 0 ? lane : lane - d);
+    const int y = __shfl(incl, lane - d < 0 ? lane : lane - d);
     if (lane >= d) incl += y;
   }
   if (lane == 63) lds.sums[wave] = incl;
   __syncthreads();
   Share r{};
-  long long base = 0;
-  for (int w = 0; w < THREADS / 64; ++w) {
+  int base = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
     if (w == wave) base = r.total;
     r.total += lds.sums[w];
   }
+  r.total = __builtin_amdgcn_readfirstlane(r.total);
   base += incl - mine;
-  r.active = (int)min((long long)gridDim.x, r.total);
+  r.active = min((int)gridDim.x, r.total);
   r.index = blockIdx.x;
-  r.idle = r.index >= r.active;
+  bool idle = r.index >= r.active;
   if (gridDim.x % kQueues == 0) {
-    const int xcd = r.index % kQueues, first = xcd * r.active / kQueues;
-    r.index = first + r.index / kQueues;
-    r.idle = r.index >= (xcd + 1) * r.active / kQueues;
+    const int xcd = r.index % kQueues;
+    r.index = xcd * r.active / kQueues + r.index / kQueues;
+    idle = r.index >= (xcd + 1) * r.active / kQueues;
   }
-  if (r.idle) return r;
-  r.begin = r.index * r.total / r.active;
-  r.end = (r.index + 1) * r.total / r.active;
-  if (base <= r.begin && r.begin < base + mine) {  // one thread
-    int s = s_lo;
-    for (;; ++s) {
-      const long long u = units_of<ROWS>(p, lens_of(p, s));
-      if (r.begin < base + u) break;
-      base += u;
+  if (idle) return r;
+  const int at[2] = {cut(r.index, r.total, r.active), cut(r.index + 1, r.total, r.active)};
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    if (base <= at[e] && at[e] < base + mine) {  // one thread, or none (the end of the batch)
+      int s = s_lo, before = base;
+      for (; per > 1; ++s) {
+        n = lens_of(p, s);
+        const int u = units_of<ROWS>(p, n);
+        if (at[e] < before + u) break;
+        before += u;
+      }
+      lds.seq[e] = s;
+      lds.base[e] = before;
+      lds.n[e] = n;
     }
-    lds.seq = s;
-    lds.base = base;
   }
   __syncthreads();
-  r.seq = __builtin_amdgcn_readfirstlane(lds.seq);
-  r.seq_base = lds.base;
+  r.seq = __builtin_amdgcn_readfirstlane(lds.seq[0]);
+  r.seq_base = __builtin_amdgcn_readfirstlane(lds.base[0]);
+  r.n = Lens{__builtin_amdgcn_readfirstlane(lds.n[0].prefix), __builtin_amdgcn_readfirstlane(lds.n[0].count), __builtin_amdgcn_readfirstlane(lds.n[0].first)};
+  auto snapped = [&](int x, int seq_base, int units) { return snap(x, x - (int)((unsigned)(x - seq_base) % (unsigned)units), units); };
+  r.begin = snapped(at[0], r.seq_base, key_units(p, r.n));
+  r.end = at[1];
+  if (at[1] < r.total) {
+    const Lens m{__builtin_amdgcn_readfirstlane(lds.n[1].prefix), __builtin_amdgcn_readfirstlane(lds.n[1].count), 0};
+    r.end = snapped(at[1], __builtin_amdgcn_readfirstlane(lds.base[1]), key_units(p, m));
+  }
   return r;
 }
 
@@ -193,16 +239,15 @@ __device__ __forceinline__ Share find_share(const TreeParams& p, ShareLds<THREAD
 struct Piece {
   Lens n;
   int seq, kv_head, unit, key_begin, key_end, kv_len, row0, n_rows;
-  long long item_end;
+  int item_end;
   bool whole;  // all units of the row tile
 };
 struct Walk {
   Share sh;
-  long long seq_base, at;
-  int seq;
+  int seq_base, at, seq;
   Lens n;
 };
-__device__ __forceinline__ Walk begin_walk(const TreeParams& p, const Share& sh) { return Walk{sh, sh.seq_base, sh.begin, sh.seq, lens_of(p, sh.seq)}; }
+__device__ __forceinline__ Walk begin_walk(const Share& sh) { return Walk{sh, sh.seq_base, sh.begin, sh.seq, sh.n}; }
 template <int ROWS>
 __device__ __forceinline__ bool next_piece(const TreeParams& p, Walk& w, Piece& it) {
   if (w.at >= w.sh.end) return false;
@@ -210,20 +255,18 @@ __device__ __forceinline__ bool next_piece(const TreeParams& p, Walk& w, Piece& 
     w.seq_base += units_of<ROWS>(p, w.n);
     w.n = lens_of(p, ++w.seq);
   }
-  const int n_key_units = key_units(w.n), n_tiles = row_tiles<ROWS>(p, w.n);
-  const long long rel = w.at - w.seq_base;
-  const int tile_index = (int)(rel / n_key_units);
+  const unsigned n_key_units = key_units(p, w.n), n_tiles = row_tiles<ROWS>(p, w.n), rel = w.at - w.seq_base, tile_index = rel / n_key_units;
   it.n = w.n;
   it.seq = w.seq;
-  it.unit = (int)(rel - (long long)tile_index * n_key_units);
+  it.unit = rel - tile_index * n_key_units;
   it.kv_head = tile_index / n_tiles;
   it.row0 = (tile_index - it.kv_head * n_tiles) * ROWS;
   it.n_rows = min(ROWS, w.n.count * (p.n_q_heads / p.n_kv_heads) - it.row0);
-  it.item_end = w.at - it.unit + n_key_units;
-  const long long end = min(it.item_end, w.sh.end);
+  it.item_end = w.at - it.unit + (int)n_key_units;
+  const int end = min(it.item_end, w.sh.end);
   it.kv_len = w.n.prefix + w.n.count;
-  it.key_begin = it.unit * kUnitKeys;
-  it.key_end = min(it.kv_len, (it.unit + (int)(end - w.at)) * kUnitKeys);
+  it.key_begin = it.unit * p.unit_keys;
+  it.key_end = end == it.item_end ? it.kv_len : (it.unit + end - w.at) * p.unit_keys;
   it.whole = it.unit == 0 && end == it.item_end;
   w.at = end;
   return true;
@@ -232,7 +275,7 @@ __device__ __forceinline__ bool next_piece(const TreeParams& p, Walk& w, Piece& 
 __device__ __forceinline__ void note_split(const TreeParams& p, const Share& sh, const Piece& it) {
   if (it.unit != 0 || it.whole || threadIdx.x != 0) return;
   int last = sh.index + 1;
-  while ((last + 1) * sh.total / sh.active < it.item_end) ++last;
+  while (cut(last + 1, sh.total, sh.active) + kSnapUnits < it.item_end) ++last;
   p.splits[blockIdx.x] = Split{last - sh.index + 1, sh.index, it.n_rows, it.row0, it.kv_head, it.n.first, it.n.prefix, it.n.count};
 }
 
@@ -406,28 +449,29 @@ __device__ __forceinline__ void join_and_store(const TreeParams& p, const Piece&
 }
 
 // ------------------------------------------------------------------------------------------------------------ few rows
-template <int D, bool FP8, int WR>
+template <int D, bool FP8>
 __global__ __launch_bounds__(kThreads, 2) void stream_kernel(TreeParams p) {
-  constexpr int NSTEP = D / 16, NDB = D / 32, ESZ = FP8 ? 1 : 2, WK = kWaves / WR, ROWS = 32 * WR;
+  constexpr int NSTEP = D / 16, NDB = D / 32, ESZ = FP8 ? 1 : 2, WK = kWaves, ROWS = 32;
   constexpr int BLKB = 16 * D * ESZ;                            // bytes of one (block, head) of the cache
   constexpr int WAVE_LDS = 2 * NSTEP * 1024 + (FP8 ? 512 : 0);  // a wave's K and V planes, or two sets of block images (fp8)
   static_assert(WAVE_LDS >= 32 * D * 4, "a wave's result takes the place of its planes");
   __shared__ __align__(1024) unsigned char smem[kWaves * WAVE_LDS];
   __shared__ float ml_lds[kWaves][32][2];
-  __shared__ ShareLds<kThreads> share_lds;
+  __shared__ ShareLds share_lds;
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31, pr = perm32(c32);
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = p.n_q_heads / p.n_kv_heads;
   const Share sh = find_share<ROWS>(p, share_lds);
   if (tid == 0) p.splits[blockIdx.x].n_pieces = 0;
-  if (sh.idle) return;
-  Walk walk = begin_walk(p, sh);
+  if (sh.begin >= sh.end) return;
+  const bool big = (long long)sh.total * p.unit_keys * (2 * D * ESZ) >= kPastCacheBytes;
+  Walk walk = begin_walk(sh);
   Piece it;
   while (next_piece<ROWS>(p, walk, it)) {
     Rows<D> rows;
     rows.clear();
-    const int row = min(it.row0 + wr * 32 + c32, it.n.count * group - 1);
+    const int row = min(it.row0 + c32, it.n.count * group - 1);
     rows.token = row / group;
     unsigned flip;
     const float c = score_factor<FP8>(p, it.kv_head, flip);
@@ -465,19 +509,26 @@ __global__ __launch_bounds__(kThreads, 2) void stream_kernel(TreeParams p) {
       if (odd) add_odd_values<D, FP8>(p, it, rows, pp, key, half, c32);
     };
 
-    // Sub-tiles wk, wk + WK, ... of the piece; table entries of the next 32 of them in one register, two lanes each.
+    // Sub-tiles wave, wave + 8, ... of the piece; table entries of the next 32 of them in one register, two lanes each.
     const int* table = p.block_tables + (long long)it.seq * p.max_blocks;
     const int last_block = (it.kv_len - 1) / kBlock;
     int bt_reg = 0;
     auto load_table = [&](int j0) {
-      const int u = wk + WK * (j0 + (lane >> 1));
+      const int u = wave + WK * (j0 + (lane >> 1));
       bt_reg = table[min((it.key_begin + 32 * u) / kBlock + (lane & 1), last_block)];
     };
     auto pin_table = [&]() { asm volatile("" : "+v"(bt_reg)); };
     const int n_sub = (it.key_end - it.key_begin + 31) / 32;
-    const int n_iter = n_sub > wk ? (n_sub - wk + WK - 1) / WK : 0;
+    const int n_iter = n_sub > wave ? (n_sub - wave + WK - 1) / WK : 0;
     lds_byte* wl = (lds_byte*)smem + wave * WAVE_LDS;
     const unsigned wl_addr = (unsigned)(unsigned long long)wl;
+    // K/V that one item reads, and much of it in the batch, keeps out of the caches (kPastCacheBytes): 64 single tokens behind 256 .. 8000 keys
+    // 221 us a pass, 197 past the caches.
+    const bool past_cache = it.n_rows == it.n.count * group && big;
+    auto stream = [&](auto run) -> void {
+      if (past_cache) run(std::integral_constant<int, kNonTemporal>{});
+      else run(std::integral_constant<int, 0>{});
+    };
     load_table(0);
 #pragma unroll
     for (int st = 0; st < NSTEP; ++st) qraw[st] = *reinterpret_cast<const u32x4*>(qp + 16 * st);
@@ -485,55 +536,57 @@ __global__ __launch_bounds__(kThreads, 2) void stream_kernel(TreeParams p) {
     if constexpr (!FP8) {
       const unsigned rd = wl_addr + lane * 16;  // each lane reads back the chunks that it fetched
       const int k_off = (half * 16 + (pr & 15)) * 16, v_off = (half * D + pr) * 16;
-      auto issue_k = [&](int j) {
+      auto issue_k = [&](auto nt, int j) -> void {
         const long long b0 = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31)), b1 = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + 1);
         const unsigned char* g = p.k_pool + (((pr >> 4) ? b1 : b0) * p.n_kv_heads + it.kv_head) * BLKB + k_off;
 #pragma unroll
-        for (int st = 0; st < NSTEP; ++st) __builtin_amdgcn_global_load_lds(g + st * 512, wl + st * 1024, 16, 0, 0);
+        for (int st = 0; st < NSTEP; ++st) __builtin_amdgcn_global_load_lds(g + st * 512, wl + st * 1024, 16, 0, decltype(nt)::value);
       };
-      auto issue_v = [&](int j) {
+      auto issue_v = [&](auto nt, int j) -> void {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const long long b = __builtin_amdgcn_readlane(bt_reg, 2 * (j & 31) + t);
           const unsigned char* g = p.v_pool + (b * p.n_kv_heads + it.kv_head) * BLKB + v_off;
 #pragma unroll
-          for (int db = 0; db < NDB; ++db) __builtin_amdgcn_global_load_lds(g + db * 512, wl + (NSTEP + t * NDB + db) * 1024, 16, 0, 0);
+          for (int db = 0; db < NDB; ++db) __builtin_amdgcn_global_load_lds(g + db * 512, wl + (NSTEP + t * NDB + db) * 1024, 16, 0, decltype(nt)::value);
         }
       };
-      if (n_iter > 0) {
-        issue_k(0);
-        issue_v(0);
-      }
-      pin_q();
-      for (int j = 0; j < n_iter; ++j) {
-        const int key = it.key_begin + 32 * (wk + WK * j);
-        const bool more = j + 1 < n_iter;
-        u32x4 kop[NSTEP], vop[NSTEP], pp[2];
-        f32x16 sc;
-        wait_vmcnt<NSTEP>();  // K(j) has landed; the V(j) loads behind it may still fly
-        lds_read_planes<NSTEP>(kop, rd);
-        scores(kop, sc);
-        if (more) {
-          if (((j + 1) & 31) == 0) {
-            load_table(j + 1);
-            pin_table();
-          }
-          issue_k(j + 1);
+      stream([&](auto nt) -> void {
+        if (n_iter > 0) {
+          issue_k(nt, 0);
+          issue_v(nt, 0);
         }
-        weights(sc, key, pp);
-        if (more) wait_vmcnt<NSTEP>();
-        else wait_vmcnt<0>();  // V(j) has landed
-        lds_read_planes<NSTEP>(vop, rd + NSTEP * 1024);
-        sums(vop, pp, key);
-        if (more) issue_v(j + 1);
-      }
+        pin_q();
+        for (int j = 0; j < n_iter; ++j) {
+          const int key = it.key_begin + 32 * (wave + WK * j);
+          const bool more = j + 1 < n_iter;
+          u32x4 kop[NSTEP], vop[NSTEP], pp[2];
+          f32x16 sc;
+          wait_vmcnt<NSTEP>();  // K(j) has landed; the V(j) loads behind it may still fly
+          lds_read_planes<NSTEP>(kop, rd);
+          scores(kop, sc);
+          if (more) {
+            if (((j + 1) & 31) == 0) {
+              load_table(j + 1);
+              pin_table();
+            }
+            issue_k(nt, j + 1);
+          }
+          weights(sc, key, pp);
+          if (more) wait_vmcnt<NSTEP>();
+          else wait_vmcnt<0>();  // V(j) has landed
+          lds_read_planes<NSTEP>(vop, rd + NSTEP * 1024);
+          sums(vop, pp, key);
+          if (more) issue_v(nt, j + 1);
+        }
+      });
     } else {
       // The two blocks of a sub-tile are copied whole (K: the second image 128 bytes further, so that the halves of a read hit
       // different banks), the operands' 8-byte chunks picked out of the images and converted.  Two sets.
       constexpr int NIB = BLKB / 1024, NIK = 2 * NIB, KSET = 2 * BLKB + 128, SET = KSET + 2 * BLKB;
       static_assert(2 * SET <= WAVE_LDS, "two sets per wave");
       const unsigned k_rd = wl_addr + (pr >> 4) * (BLKB + 128) + (half * 16 + (pr & 15)) * 8, v_rd = wl_addr + KSET + (half * D + pr) * 8;
-      auto issue = [&](int j) {
+      auto issue = [&](auto nt, int j) -> void {
         if (j && (j & 31) == 0) {
           load_table(j);
           pin_table();
@@ -545,35 +598,37 @@ __global__ __launch_bounds__(kThreads, 2) void stream_kernel(TreeParams p) {
           const unsigned char* g = (x < 2 ? p.k_pool : p.v_pool) + (b * p.n_kv_heads + it.kv_head) * BLKB + lane * 16;
 #pragma unroll
           for (int i = 0; i < NIB; ++i)
-            __builtin_amdgcn_global_load_lds(g + i * 1024, set + (x < 2 ? x * (BLKB + 128) : KSET + (x - 2) * BLKB) + i * 1024, 16, 0, 0);
+            __builtin_amdgcn_global_load_lds(g + i * 1024, set + (x < 2 ? x * (BLKB + 128) : KSET + (x - 2) * BLKB) + i * 1024, 16, 0, decltype(nt)::value);
         }
       };
-      if (n_iter > 0) issue(0);
-      if (n_iter > 1) issue(1);
-      pin_q();
-      for (int j = 0; j < n_iter; ++j) {
-        const int key = it.key_begin + 32 * (wk + WK * j);
-        const bool more = j + 1 < n_iter;  // sub-tile j + 1 has been requested
-        u32x4 kop[NSTEP], vop[NSTEP], pp[2];
-        u32x2 codes[NSTEP];
-        f32x16 sc;
-        if (more) wait_vmcnt<3 * NIK>();
-        else wait_vmcnt<NIK>();  // K(j) has landed
-        if constexpr (NSTEP == 8) lds_read8_b64<0, 256, 512, 768, 1024, 1280, 1536, 1792>(codes, k_rd + (j & 1) * SET);
-        else lds_read4_b64<0, 256, 512, 768>(codes, k_rd + (j & 1) * SET);
-#pragma unroll
-        for (int x = 0; x < NSTEP; ++x) kop[x] = fp8x8_to_bf16x8(codes[x]);
-        scores(kop, sc);
-        weights(sc, key, pp);
-        if (more) wait_vmcnt<2 * NIK>();
-        else wait_vmcnt<0>();  // V(j) has landed
-        if constexpr (NSTEP == 8) lds_read8_b64<0, 256, 512, 768, BLKB, BLKB + 256, BLKB + 512, BLKB + 768>(codes, v_rd + (j & 1) * SET);
-        else lds_read4_b64<0, 256, BLKB, BLKB + 256>(codes, v_rd + (j & 1) * SET);
-        if (j + 2 < n_iter) issue(j + 2);  // the set is free again
-#pragma unroll
-        for (int x = 0; x < NSTEP; ++x) vop[x] = fp8x8_to_bf16x8(codes[x]);
-        sums(vop, pp, key);
-      }
+      stream([&](auto nt) -> void {
+        if (n_iter > 0) issue(nt, 0);
+        if (n_iter > 1) issue(nt, 1);
+        pin_q();
+        for (int j = 0; j < n_iter; ++j) {
+          const int key = it.key_begin + 32 * (wave + WK * j);
+          const bool more = j + 1 < n_iter;  // sub-tile j + 1 has been requested
+          u32x4 kop[NSTEP], vop[NSTEP], pp[2];
+          u32x2 codes[NSTEP];
+          f32x16 sc;
+          if (more) wait_vmcnt<3 * NIK>();
+          else wait_vmcnt<NIK>();  // K(j) has landed
+          if constexpr (NSTEP == 8) lds_read8_b64<0, 256, 512, 768, 1024, 1280, 1536, 1792>(codes, k_rd + (j & 1) * SET);
+          else lds_read4_b64<0, 256, 512, 768>(codes, k_rd + (j & 1) * SET);
+  #pragma unroll
+          for (int x = 0; x < NSTEP; ++x) kop[x] = fp8x8_to_bf16x8(codes[x]);
+          scores(kop, sc);
+          weights(sc, key, pp);
+          if (more) wait_vmcnt<2 * NIK>();
+          else wait_vmcnt<0>();  // V(j) has landed
+          if constexpr (NSTEP == 8) lds_read8_b64<0, 256, 512, 768, BLKB, BLKB + 256, BLKB + 512, BLKB + 768>(codes, v_rd + (j & 1) * SET);
+          else lds_read4_b64<0, 256, BLKB, BLKB + 256>(codes, v_rd + (j & 1) * SET);
+          if (j + 2 < n_iter) issue(nt, j + 2);  // the set is free again
+  #pragma unroll
+          for (int x = 0; x < NSTEP; ++x) vop[x] = fp8x8_to_bf16x8(codes[x]);
+          sums(vop, pp, key);
+        }
+      });
     }
 
     put_result<D>(smem + wave * WAVE_LDS, c32, rows.o, half);
@@ -597,24 +652,24 @@ __global__ __launch_bounds__(kThreads, 2) void tiles_kernel(TreeParams p) {
   constexpr int NSTEP = D / 16, NDB = D / 32, ESZ = FP8 ? 1 : 2, WK = kWaves / WR, ROWS = 32 * WR;
   constexpr int BLKB = 16 * D * ESZ;
   constexpr int PIECES = 4 * D;                           // of K and V of a block: 8 elements each, 16 bytes in LDS
-  constexpr int TILE = kUnitKeys / kBlock * PIECES * 16;  // bytes of a tile
+  constexpr int TILE = kTileKeys / kBlock * PIECES * 16;  // bytes of a tile
   constexpr int PER = TILE / 16 / kThreads;               // pieces of a thread
-  constexpr int kTiles = 2, SUBS = kUnitKeys / 32 / WK;   // tiles in LDS; a wave's sub-tiles of one: wk, wk + WK, ...
+  constexpr int kTiles = 2, SUBS = kTileKeys / 32 / WK;   // tiles in LDS; a wave's sub-tiles of one: wk, wk + WK, ...
   static_assert(SUBS >= 1, "a sub-tile for every wave");
   constexpr int RESULT = 32 * D * 4;
   constexpr int LDS = WK > 1 && kWaves * RESULT > kTiles * TILE ? kWaves * RESULT : kTiles * TILE;
   using Codes = std::conditional_t<FP8, u32x2, u32x4>;
   __shared__ __align__(1024) unsigned char smem[LDS];
   __shared__ float ml_lds[WK > 1 ? kWaves : 1][32][2];
-  __shared__ ShareLds<kThreads> share_lds;
+  __shared__ ShareLds share_lds;
 
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, c32 = lane & 31, pr = perm32(c32);
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
   const int group = p.n_q_heads / p.n_kv_heads;
   const Share sh = find_share<ROWS>(p, share_lds);
   if (tid == 0) p.splits[blockIdx.x].n_pieces = 0;
-  if (sh.idle) return;
-  Walk walk = begin_walk(p, sh);
+  if (sh.begin >= sh.end) return;
+  Walk walk = begin_walk(sh);
   Piece it;
   while (next_piece<ROWS>(p, walk, it)) {
     Rows<D> rows;
@@ -625,12 +680,12 @@ __global__ __launch_bounds__(kThreads, 2) void tiles_kernel(TreeParams p) {
     const float c = score_factor<FP8>(p, it.kv_head, flip);
     const int* table = p.block_tables + (long long)it.seq * p.max_blocks;
     const int last_block = (it.kv_len - 1) / kBlock;
-    const int n_tiles = (it.key_end - it.key_begin + kUnitKeys - 1) / kUnitKeys;
+    const int n_tiles = (it.key_end - it.key_begin + kTileKeys - 1) / kTileKeys;
 
     // Table entries of 16 tiles in one register, a lane each, and of the 16 after them: an entry is there when its block is
     // requested (loaded with each tile, they cost it their round trip).
-    constexpr int kAhead = 64 * kBlock / kUnitKeys;
-    auto load_table = [&](int j) { return table[min(it.key_begin / kBlock + j * (kUnitKeys / kBlock) + lane, last_block)]; };
+    constexpr int kAhead = 64 * kBlock / kTileKeys;
+    auto load_table = [&](int j) { return table[min(it.key_begin / kBlock + j * (kTileKeys / kBlock) + lane, last_block)]; };
     int entries = load_table(0), entries_next = 0;
     if (n_tiles > kAhead) entries_next = load_table(kAhead);
     Codes r[PER];
@@ -642,7 +697,7 @@ __global__ __launch_bounds__(kThreads, 2) void tiles_kernel(TreeParams p) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int x = i * kThreads + tid, b = __builtin_amdgcn_readfirstlane(x / PIECES), in = x % PIECES;
-        const long long block = __builtin_amdgcn_readlane(entries, (j % kAhead) * (kUnitKeys / kBlock) + b);
+        const long long block = __builtin_amdgcn_readlane(entries, (j % kAhead) * (kTileKeys / kBlock) + b);
         const unsigned char* pool = __builtin_amdgcn_readfirstlane(in / (PIECES / 2)) ? p.v_pool : p.k_pool;
         r[i] = *reinterpret_cast<const Codes*>(pool + (block * p.n_kv_heads + it.kv_head) * BLKB + in % (PIECES / 2) * (8 * ESZ));
       }
@@ -671,7 +726,7 @@ __global__ __launch_bounds__(kThreads, 2) void tiles_kernel(TreeParams p) {
       __syncthreads();
 #pragma unroll
       for (int x = 0; x < SUBS; ++x) {
-        const int key = it.key_begin + j * kUnitKeys + 32 * (wk + WK * x);
+        const int key = it.key_begin + j * kTileKeys + 32 * (wk + WK * x);
         if (key >= it.key_end) break;
         const unsigned char* lds = buffer + 2 * (wk + WK * x) * (PIECES * 16);
         u32x4 kop[NSTEP], vop[NSTEP], pp[2];
@@ -764,19 +819,25 @@ __global__ __launch_bounds__(256) void merge_kernel(TreeParams p) {
   *reinterpret_cast<u32x2*>(p.out + ((long long)(sp.first_token + token) * p.n_q_heads + head) * D + d) = w;
 }
 
-// Rows of a tile: as many as it takes for a sequence's rows of a KV head, up to 256.
-int rows_of_tile(const cronus_kv_cache* cache, int32_t max_rows) {
+int most_rows_of_tile(const cronus_kv_cache* cache, int32_t max_rows) {
   const long long rows = (long long)max_rows * (cache->num_q_heads / cache->num_kv_heads);
-  return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  return rows <= 32 ? 32 : rows <= 192 ? 128 : 256;
+}
+int rows_of_tile(const cronus_kv_cache* cache, int32_t max_rows, int32_t n_seqs) {
+  const long long rows = (long long)max_rows * (cache->num_q_heads / cache->num_kv_heads);
+  const double tiles = (double)((rows + 31) / 32) * cache->num_kv_heads * n_seqs;  // (a product of three counts)
+  const int most = most_rows_of_tile(cache, max_rows);
+  return tiles <= kFewRowTiles ? 32 : tiles < kManyRowTiles ? std::min(most, 128) : most;
 }
 
 size_t split_bytes(int n_cus) { return ((size_t)n_cus * sizeof(Split) + 255) / 256 * 256; }
 
 template <int D, bool FP8, int ROWS>
 int launch(const TreeParams& p, int n_cus, hipStream_t stream) {
-  if constexpr (ROWS <= 64) hipLaunchKernelGGL((stream_kernel<D, FP8, ROWS / 32>), dim3(n_cus), dim3(kThreads), 0, stream, p);
+  if constexpr (ROWS == 32) hipLaunchKernelGGL((stream_kernel<D, FP8>), dim3(n_cus), dim3(kThreads), 0, stream, p);
   else hipLaunchKernelGGL((tiles_kernel<D, FP8, ROWS / 32>), dim3(n_cus), dim3(kThreads), 0, stream, p);
   if (hipGetLastError() != hipSuccess) return CRONUS_ERR_HIP;
+  if (p.whole) return CRONUS_OK;  // no row tile is split
   hipLaunchKernelGGL((merge_kernel<D, FP8, ROWS>), dim3(n_cus, ROWS * D / 1024), dim3(256), 0, stream, p);
   return hipGetLastError() == hipSuccess ? CRONUS_OK : CRONUS_ERR_HIP;
 }
@@ -784,7 +845,6 @@ template <int D, bool FP8>
 int launch_rows(const TreeParams& p, int rows, int n_cus, hipStream_t stream) {
   switch (rows) {
     case 32: return launch<D, FP8, 32>(p, n_cus, stream);
-    case 64: return launch<D, FP8, 64>(p, n_cus, stream);
     case 128: return launch<D, FP8, 128>(p, n_cus, stream);
     default: return launch<D, FP8, 256>(p, n_cus, stream);
   }
@@ -793,7 +853,7 @@ int launch_rows(const TreeParams& p, int rows, int n_cus, hipStream_t stream) {
 }  // namespace
 
 size_t attn_tree_workspace(const cronus_kv_cache* cache, int32_t max_rows, int n_cus) {
-  const size_t slot = (size_t)rows_of_tile(cache, max_rows) * (cache->head_dim + 2) * sizeof(float);
+  const size_t slot = (size_t)most_rows_of_tile(cache, max_rows) * (cache->head_dim + 2) * sizeof(float);
   return split_bytes(n_cus) + (2 * slot * n_cus + 255) / 256 * 256;
 }
 
@@ -820,7 +880,16 @@ int launch_attn_tree(const cronus_kv_cache* cache, const void* q, void* out, con
   p.scale_log2e = sm_scale * 1.4426950408889634f;
   p.splits = static_cast<Split*>(workspace);
   p.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + split_bytes(n_cus));
-  const int rows = rows_of_tile(cache, max_rows);
+  const int rows = rows_of_tile(cache, max_rows, n_seqs);
+  const double tiles = (double)(((long long)max_rows * (p.n_q_heads / p.n_kv_heads) + rows - 1) / rows) * p.n_kv_heads * n_seqs;
+  const long long keys = (long long)max_blocks_per_seq * kBlock, step = rows == 32 ? 32 * kWaves : kTileKeys;  // one sub-tile or more for every wave
+  long long unit_keys = step;
+  p.whole = keys <= kWholeSteps * step;
+  if (p.whole) unit_keys = (keys + step - 1) / step * step;
+  auto too_many = [&] { return tiles * (double)((keys + unit_keys - 1) / unit_keys) >= (double)(kMostUnitShares / n_cus); };
+  while (too_many() && unit_keys < kTreeMostKeys / 4) unit_keys *= 2;
+  if (too_many()) return CRONUS_ERR_INVALID_ARG;
+  p.unit_keys = (int)unit_keys;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool fp8 = cache->kv_dtype == CRONUS_KV_FP8_E4M3;
   if (cache->head_dim == 128) return fp8 ? launch_rows<128, true>(p, rows, n_cus, s) : launch_rows<128, false>(p, rows, n_cus, s);

@@ -50,6 +50,8 @@ def test_attn_tree_refusals():
     assert sizes == sorted(sizes)
     for kw in (dict(ws=None), dict(ws=FAKE + 8), dict(ws_bytes=need - 1), dict(ws_bytes=0)):
         assert tree(**kw) == WORKSPACE, kw
+    for kw in (dict(n=0x7FFFFFFF), dict(n=0x7FFFFFFF, rows=0x0FFFFFF, mask=None), dict(n=0x7FFFFFFF, rows=1, cache=cache(hq=0x7FFFFFFF, hkv=0x7FFFFFFF))):
+        assert tree(ws_bytes=1 << 40, **kw) == BAD, kw  # more row tiles than shares are counted in
     assert tree(n=0, q=None, ws=None) == B.CRONUS_OK and tree(rows=0, q=None, ws=None) == B.CRONUS_OK
     if no_gpu():
         assert tree(ws_bytes=need) == B.CRONUS_ERR_HIP
