@@ -5,16 +5,20 @@
 // The host does not know the lengths, so a launch has as many work-groups as the GPU has CUs, and each finds its share itself: the
 // batch is a sequence of U units (a row tile of a KV head against unit_keys keys; keys run fastest, then row tiles, heads, sequences),
 // and share l of A = min(work-groups, U) is units [l U / A, (l + 1) U / A), at least one.  Neighbouring shares, whose row tiles read the same
-// keys, go to one XCD.  A row tile whose units lie in several shares is left as partial results (m, l, O), which
+// keys, go to one XCD (and a cut close to the end of an item moves there).  A row tile whose units lie in several shares is left as partial results (m, l, O), which
 // merge_kernel combines; a share has at most two of them, one at either end, so the workspace does not depend on the lengths.
 //
 // S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: a row (a drafted token and a query head of the KV head) is a column, its
-// lanes are l and l + 32, and P stays in registers.  Two kernels, by the rows of a KV head that a sequence can have:
-//   stream_kernel - few rows, bound by memory: 8 wavefronts, WR side by side with 32 rows each, 8 / WR of which take every (8 / WR)-th
-//                   32-key sub-tile.  Each moves its own sub-tiles to LDS of its own, by DMA: loads in flight take no registers, and no
-//                   wave waits for another.
-//   tiles_kernel  - many rows, bound by products: the same waves, but tiles of kTileKeys keys go through registers (fp8 codes are
-//                   converted there, once) to one of two LDS buffers, where all waves read their operands.
+// lanes are l and l + 32, and P stays in registers.  Two kernels of 8 wavefronts:
+//   stream_kernel - row tiles of 32, bound by memory: every wavefront has all 32 rows and takes every eighth sub-tile of 32 keys, which it
+//                   moves to LDS of its own, by DMA: loads in flight take no registers, and no wave waits for another.  The eight results are
+//                   joined in LDS.
+//   tiles_kernel  - row tiles of 128 or 256, bound by what a CU issues: a wavefront has 32 of the rows.  Tiles of kTileKeys keys go through registers
+//                   (fp8 codes are converted there, once) to one of two LDS buffers, where all waves read their operands.
+// What the second one is at: 16 trees of 48 .. 61 tokens, 8 heads a KV head, fp8, behind 8000 .. 32000 keys take 690 .. 720 us, 0.80 PFLOP/s (0.95 with
+// the empty rows of its tiles); the matrix pipes are busy for 41 % of it, a wave issues for 35 % and waits for LDS, memory or the barrier for 38 %, LDS moves
+// for 26 %.  Tried, within 2 % of it or slower: V and the next K read a step ahead; scores of the next sub-tile between the numerators of this one; the
+// two waves of a SIMD half a step apart; s_setprio around the products; bf16 tiles by DMA in a ring of four (204 -> 225 us, 32 trees of 64).
 #include <hip/hip_runtime.h>
 #include <algorithm>
 
@@ -35,14 +39,16 @@ constexpr long long kFewRowTiles = 352, kManyRowTiles = 1536;
 // keys and 21 tokens, 7 heads a KV head, 24.2 / 21.7 / 22.2; fp8, 13 of 56 .. 3028 and 4 .. 33 46.3 / 41.2 / 41.0; 9 of 106 .. 10230 66.8 / 60.6 / 60.5; 25 chains
 // of 500 .. 4097 35.5 / 36.0 / 39.2 (and with 3, 32 trees of 64 213 instead of 204).
 constexpr int kSnapUnits = 1;
-// Where the tables have room for so many steps of a work-group at most (1792 keys streamed, 448 in tiles), a unit holds all keys of a
+// Where the tables have room for so many steps of a work-group at most (1792 keys streamed, 896 in tiles), a unit holds all keys of a
 // sequence: no row tile is split, so there is no merge launch, and every work-group has whole items.  us a pass, cut / whole: a tree of 8 behind
 // 256 keys 12.5 / 9.5; 31 single tokens behind 40 .. 346 19.2 / 11.6; 11 trees of 5 .. 28, fp8, behind 17 .. 700 19.8 / 13.1; 166 single tokens behind
 // 52 .. 1162 106.6 / 94.9.  With 12 steps 8 trees of 12 .. 32 behind 200 .. 3000 take 27.9 instead of 30.2, but 146 single tokens behind
 // 398 .. 3011, 7 heads a KV head, 112.7 instead of 90.2.
 constexpr int kWholeSteps = 7;
 constexpr int kNonTemporal = 2;  // cache policy operand of a transfer: the instruction's nt bit
-constexpr int kTileKeys = 64;             // of a tile in LDS (tiles_kernel)
+// Of a tile in LDS (tiles_kernel).  us a pass, 64 / 128: 16 trees of 48 .. 61, fp8, 742 / 714; a whole iteration with 24 trees 96 / 92; two K
+// and V buffers of 256 keys do not fit.
+constexpr int kTileKeys = 128;
 // Units times work-groups stay below this, for any lengths that the tables have room for: shares are computed in 32 bits, where a 64-bit
 // division is 140 instructions.
 constexpr long long kMostUnitShares = 1LL << 31;
@@ -727,7 +733,7 @@ __global__ __launch_bounds__(kThreads, 2) void tiles_kernel(TreeParams p) {
 #pragma unroll
       for (int x = 0; x < SUBS; ++x) {
         const int key = it.key_begin + j * kTileKeys + 32 * (wk + WK * x);
-        if (key >= it.key_end) break;
+        if (key >= it.key_end || wr * 32 >= it.n_rows) break;  // a wave without rows only moves tiles (34 trees of 112 .. 264 rows 574 / 529)
         const unsigned char* lds = buffer + 2 * (wk + WK * x) * (PIECES * 16);
         u32x4 kop[NSTEP], vop[NSTEP], pp[2];
         f32x16 sc;
