@@ -323,7 +323,7 @@ typedef struct cronus_paged_tables {
  * was asked for (0 lengths aside), block_tables, free_blocks, held and the count stay as they were, cu_tokens and cu_blocks are all 0 and start_pos is kv_lens: the
  * calls that take them then do nothing.
  * Outputs must not overlap inputs or one another, but for the pairs named above.
- * Errors: INVALID_ARG (null pointer, negative size), HIP.
+ * Errors: INVALID_ARG (null pointer, negative size, more than 2^30 sequences), HIP.
  */
 int cronus_build_tables(const cronus_paged_tables* tables, const int32_t* kv_lens, const int32_t* new_lens, int32_t n_seqs,
                         int32_t* cu_tokens, int32_t* start_pos, int32_t* cu_blocks, int64_t* slot_map, int32_t max_tokens,
@@ -361,7 +361,7 @@ size_t cronus_attn_tree_workspace_bytes(const cronus_kv_cache* cache, int32_t ma
  * cronus_kv_commit - keep the accepted drafted tokens.  In every one of n_caches caches (a model's layers: same heads, head_dim
  * and dtype, same block tables) the K/V of sequence s at position start_pos[s] + paths[s][k] move to start_pos[s] + k, for
  * k = 0 .. m - 1 in effect at once, and kv_lens_out[s] = start_pos[s] + m.
- *   caches      : host, cronus_kv_cache [n_caches]
+ *   caches      : host, cronus_kv_cache [n_caches], every cache once
  *   start_pos   : device, int32 [n_seqs]; cu_rows: device, int32 [n_seqs+1], the drafted tokens as for cronus_attn_tree
  *   paths       : device, int32 [n_seqs][max_path], accepted tokens, strictly rising (a token lies behind its parent); path_lens:
  *                 device, int32 [n_seqs].  A path ends early (m < path_lens[s]) at max_path and at the first entry that is not one of
@@ -369,7 +369,7 @@ size_t cronus_attn_tree_workspace_bytes(const cronus_kv_cache* cache, int32_t ma
  *   kv_lens_out : device, int32 [n_seqs], or NULL; must not overlap start_pos, cu_rows, paths or path_lens
  * m = 0 for a sequence whose drafted tokens do not lie in [0, 16 * max_blocks_per_seq).  The blocks from start_pos[s] on must
  * not be shared by sequences.  Bits move unchanged; all other slots keep theirs.
- * Errors: INVALID_ARG (also: caches that differ, kv_lens_out overlaps start_pos), UNSUPPORTED, HIP.
+ * Errors: INVALID_ARG (also: caches that differ, kv_lens_out overlaps an input), UNSUPPORTED, HIP.
  */
 int cronus_kv_commit(const cronus_kv_cache* caches, int32_t n_caches, const int32_t* start_pos, const int32_t* cu_rows,
                      const int32_t* paths, int32_t max_path, const int32_t* path_lens, const int32_t* block_tables,

@@ -1,17 +1,20 @@
 // C ABI entry points for drafted tokens (include/cronus.h): argument checks, launches.  Lengths are the device's to check.
 #include <cmath>
+#include <utility>
 
 #include "api_checks.h"
 #include "cronus_internal.h"
 
 using namespace cronus;
 
+static constexpr int32_t kMostTableSeqs = 1 << 30;  // sequences are counted in steps of a work-group, in 32 bits
+
 extern "C" {
 
 int cronus_build_tables(const cronus_paged_tables* tables, const int32_t* kv_lens, const int32_t* new_lens, int32_t n_seqs,
                         int32_t* cu_tokens, int32_t* start_pos, int32_t* cu_blocks, int64_t* slot_map, int32_t max_tokens,
                         int32_t* report, void* hip_stream) {
-  if (!tables || n_seqs < 0 || max_tokens < 0 || tables->max_blocks_per_seq <= 0 || tables->free_capacity < 0) return CRONUS_ERR_INVALID_ARG;
+  if (!tables || n_seqs < 0 || n_seqs > kMostTableSeqs || max_tokens < 0 || tables->max_blocks_per_seq <= 0 || tables->free_capacity < 0) return CRONUS_ERR_INVALID_ARG;
   if ((tables->free_capacity > 0 && !tables->free_blocks) || !tables->free_count || !tables->free_count_out) return CRONUS_ERR_INVALID_ARG;
   if (!cu_tokens || !cu_blocks || !report) return CRONUS_ERR_INVALID_ARG;
   if (n_seqs > 0 && (!tables->block_tables || !tables->held || !tables->held_out || !kv_lens || !new_lens || !start_pos))
@@ -56,9 +59,12 @@ int cronus_kv_commit(const cronus_kv_cache* caches, int32_t n_caches, const int3
   if (n_seqs < 0 || max_path < 0 || max_blocks_per_seq <= 0) return CRONUS_ERR_INVALID_ARG;
   if (n_seqs == 0) return CRONUS_OK;
   if (!start_pos || !cu_rows || !path_lens || !block_tables || (max_path > 0 && !paths)) return CRONUS_ERR_INVALID_ARG;
-  if (kv_lens_out) {  // start_pos is read by all work-groups while one of them writes kv_lens_out
-    const uintptr_t a = reinterpret_cast<uintptr_t>(kv_lens_out), b = reinterpret_cast<uintptr_t>(start_pos), bytes = (uintptr_t)n_seqs * sizeof(int32_t);
-    if (a < b + bytes && b < a + bytes) return CRONUS_ERR_INVALID_ARG;
+  if (kv_lens_out) {  // one work-group of a sequence writes it while others read these
+    const size_t ints = sizeof(int32_t), n = (size_t)n_seqs;
+    for (auto [p, count] : {std::pair<const int32_t*, size_t>{start_pos, n}, {cu_rows, n + 1}, {path_lens, n}, {paths, n * max_path}}) {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(kv_lens_out), b = reinterpret_cast<uintptr_t>(p);
+      if (p && a < b + count * ints && b < a + n * ints) return CRONUS_ERR_INVALID_ARG;
+    }
   }
   return launch_kv_commit(caches, n_caches, start_pos, cu_rows, paths, max_path, path_lens, block_tables, max_blocks_per_seq, n_seqs,
                           kv_lens_out, hip_stream);

@@ -69,7 +69,7 @@ def build(**kw):
 def test_build_tables_refusals():
     for name in ("bt", "held", "held_out", "free", "count", "count_out", "kv", "new", "cu", "start", "cub", "report"):
         assert build(**{name: None}) == BAD, name
-    for kw in (dict(n=-1), dict(width=0), dict(capacity=-1), dict(most=-1)):
+    for kw in (dict(n=-1), dict(n=(1 << 30) + 1), dict(width=0), dict(capacity=-1), dict(most=-1)):
         assert build(**kw) == BAD, kw
     assert B.lib().cronus_build_tables(None, FAKE, FAKE, 1, FAKE, FAKE, FAKE, None, 1, FAKE, None) == BAD
     if no_gpu():
@@ -78,7 +78,8 @@ def test_build_tables_refusals():
 
 
 def commit(**kw):
-    a = dict(caches=[cache(), cache()], start=FAKE, cu=FAKE, paths=FAKE, most=4, lens=FAKE, bt=FAKE, width=4, n=3, out=FAKE + 4096)
+    a = dict(caches=[cache(), cache()], start=FAKE, cu=FAKE + 0x1000, paths=FAKE + 0x2000, most=4, lens=FAKE + 0x3000, bt=FAKE, width=4, n=3,
+             out=FAKE + 0x4000)
     a.update(kw)
     return B.cronus_kv_commit(a["caches"], a["start"], a["cu"], a["paths"], a["most"], a["lens"], a["bt"], a["width"], a["n"], a["out"], check=False)
 
@@ -86,7 +87,8 @@ def commit(**kw):
 def test_kv_commit_refusals():
     for name in ("start", "cu", "paths", "lens", "bt"):
         assert commit(**{name: None}) == BAD, name
-    for kw in (dict(n=-1), dict(most=-1), dict(width=0), dict(caches=[]), dict(out=FAKE), dict(out=FAKE + 8), dict(out=FAKE - 8)):
+    for kw in (dict(n=-1), dict(most=-1), dict(width=0), dict(caches=[]), dict(out=FAKE), dict(out=FAKE + 8), dict(out=FAKE - 8),
+               dict(out=FAKE + 0x100C), dict(out=FAKE + 0x1000 - 8), dict(out=FAKE + 0x2000 + 44), dict(out=FAKE + 0x3008)):
         assert commit(**kw) == BAD, kw
     assert B.lib().cronus_kv_commit(None, 1, FAKE, FAKE, FAKE, 1, FAKE, FAKE, 1, 1, None, None) == BAD
     for kw, code in BAD_CACHES:
@@ -97,7 +99,7 @@ def test_kv_commit_refusals():
     assert commit(n=0, start=None) == B.CRONUS_OK
     if no_gpu():
         assert commit() == B.CRONUS_ERR_HIP and commit(out=None) == B.CRONUS_ERR_HIP
-        assert commit(most=0, paths=None) == B.CRONUS_ERR_HIP and commit(out=FAKE + 12) == B.CRONUS_ERR_HIP
+        assert commit(most=0, paths=None) == B.CRONUS_ERR_HIP and commit(out=FAKE + 12) == commit(out=FAKE + 0x1010) == commit(out=FAKE + 0x2030) == B.CRONUS_ERR_HIP
 
 
 def test_errors_are_raised_by_name():
