@@ -103,7 +103,10 @@ template <int ROWS>
 __device__ __forceinline__ int row_tiles(const TreeParams& p, const Lens& n) {
   return (n.count * (p.n_q_heads / p.n_kv_heads) + ROWS - 1) / ROWS;
 }
-__device__ __forceinline__ int key_units(const TreeParams& p, const Lens& n) { return (int)((unsigned)(n.prefix + n.count + p.unit_keys - 1) / (unsigned)p.unit_keys); }
+__device__ __forceinline__ int key_units(const TreeParams& p, const Lens& n) {
+  const unsigned unit = p.unit_keys;
+  return (int)(((unsigned)n.prefix + (unsigned)n.count + unit - 1) / unit);
+}
 template <int ROWS>
 __device__ __forceinline__ int units_of(const TreeParams& p, const Lens& n) {
   return n.count ? row_tiles<ROWS>(p, n) * key_units(p, n) * p.n_kv_heads : 0;
@@ -521,7 +524,7 @@ __global__ __launch_bounds__(kThreads, 2) void stream_kernel(TreeParams p) {
     int bt_reg = 0;
     auto load_table = [&](int j0) {
       const int u = wave + WK * (j0 + (lane >> 1));
-      bt_reg = table[min((it.key_begin + 32 * u) / kBlock + (lane & 1), last_block)];
+      bt_reg = table[min(it.key_begin / kBlock + 2 * u + (lane & 1), last_block)];  // counted in blocks: keys so far past the end pass 32 bits
     };
     auto pin_table = [&]() { asm volatile("" : "+v"(bt_reg)); };
     const int n_sub = (it.key_end - it.key_begin + 31) / 32;

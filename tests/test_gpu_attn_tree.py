@@ -297,3 +297,47 @@ def test_blocks_beyond_4_gib():
     b.call(table=torch.from_numpy(moved).to(DEV))
     torch.cuda.synchronize()
     b.check(got=b.got())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp8"])
+def test_most_keys_that_a_sequence_may_have(dt):
+    """2^31 - 256 positions, all in one block of 16: every key is there equally often, so the results are those of the block alone (the last
+    drafted token that row 0 does not see is one of 2^31).  A wave takes 2^15 sub-tiles: 2^15 additions to l, each off by 2^-24, and 2^16
+    products into an accumulator, by 2^-23 each at most; numerators are rounded to bf16 in both sums (2 * 2^-8), the output once (2^-8)."""
+    b = Batch((2, 1, 64), dt, [14], [2], 31, masks=None, q_scale=0.5)
+    b.load()
+    keys, t = 2 ** 31 - 256, b.t
+    table = torch.full((1, keys // 16), int(b.table[0, 0]), dtype=torch.int32, device=DEV)
+    prefix = torch.tensor([keys - 2], dtype=torch.int32, device=DEV)
+    B.cronus_attn_tree(b.cache, t["q"], t["out"], prefix, t["cu"], None, 0, table, keys // 16, 1, 2, b.sm_scale, t["ws"], b.ws_bytes,
+                       torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    k, v = (D.values(x, scale)[:, 0] for x, scale in zip(b.kv_bits[0], b.scales))
+    score = np.einsum("rhd,kd->rhk", orc.bf16_bits_to_f64(b.q_bits), k) * b.sm_scale
+    w = np.exp(score - score.max(-1, keepdims=True))
+    w /= w.sum(-1, keepdims=True)
+    want, size = np.einsum("rhk,kd->rhd", w, v), np.einsum("rhk,kd->rhd", w, np.abs(v))
+    got = orc.bf16_bits_to_f64(bits_from_bf16_tensor(t["out"]))
+    assert (np.abs(got - want) <= size * (2.0 ** -9 + 2.0 ** -7 + 2.0 ** -7 + 2.0 ** -8)).all()
+
+
+def test_two_calls_at_once_on_two_streams():
+    """Each with its workspace; a kernel for few rows beside one for many, split and whole."""
+    batches = [Batch("usual", "bf16", [4000, 0, 77], [20, 1, 9], 41), Batch("big", "fp8", [3000, 500], [70, 64], 42), Batch("g7", "bf16", [90] * 9, [1] * 9, 43)]
+    for b in batches:
+        b.load()
+    alone = []
+    for b in batches:
+        b.call()
+        torch.cuda.synchronize()
+        alone.append(b.t["out"].clone())
+        b.t["out"].fill_(7.25)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in batches]
+    for _ in range(5):
+        for b, s in zip(batches, streams):
+            with torch.cuda.stream(s):
+                b.call()
+    torch.cuda.synchronize()
+    for b, want in zip(batches, alone):
+        assert torch.equal(b.t["out"].view(torch.int16), want.view(torch.int16))
