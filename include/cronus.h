@@ -367,9 +367,9 @@ size_t cronus_attn_tree_workspace_bytes(const cronus_kv_cache* cache, int32_t ma
  *                 device, int32 [n_seqs].  A path ends early (m < path_lens[s]) at max_path and at the first entry that is not one of
  *                 the sequence's tokens or not behind the entry before it
  *   kv_lens_out : device, int32 [n_seqs], or NULL; must not overlap start_pos, cu_rows, paths or path_lens
- * m = 0 for a sequence whose drafted tokens do not lie in [0, 16 * max_blocks_per_seq).  The blocks from start_pos[s] on must
+ * m = 0 for a sequence whose drafted tokens do not lie in [0, 16 * max_blocks_per_seq), or in [0, 2^31 - 1).  The blocks from start_pos[s] on must
  * not be shared by sequences.  Bits move unchanged; all other slots keep theirs.
- * Errors: INVALID_ARG (also: caches that differ, kv_lens_out overlaps an input), UNSUPPORTED, HIP.
+ * Errors: INVALID_ARG (also: caches that differ or come twice, kv_lens_out overlaps an input), UNSUPPORTED, HIP.
  */
 int cronus_kv_commit(const cronus_kv_cache* caches, int32_t n_caches, const int32_t* start_pos, const int32_t* cu_rows,
                      const int32_t* paths, int32_t max_path, const int32_t* path_lens, const int32_t* block_tables,

@@ -14,7 +14,8 @@ extern "C" {
 int cronus_build_tables(const cronus_paged_tables* tables, const int32_t* kv_lens, const int32_t* new_lens, int32_t n_seqs,
                         int32_t* cu_tokens, int32_t* start_pos, int32_t* cu_blocks, int64_t* slot_map, int32_t max_tokens,
                         int32_t* report, void* hip_stream) {
-  if (!tables || n_seqs < 0 || n_seqs > kMostTableSeqs || max_tokens < 0 || tables->max_blocks_per_seq <= 0 || tables->free_capacity < 0) return CRONUS_ERR_INVALID_ARG;
+  if (!tables || n_seqs < 0 || n_seqs > kMostTableSeqs || max_tokens < 0 || tables->max_blocks_per_seq <= 0 || tables->free_capacity < 0)
+    return CRONUS_ERR_INVALID_ARG;
   if ((tables->free_capacity > 0 && !tables->free_blocks) || !tables->free_count || !tables->free_count_out) return CRONUS_ERR_INVALID_ARG;
   if (!cu_tokens || !cu_blocks || !report) return CRONUS_ERR_INVALID_ARG;
   if (n_seqs > 0 && (!tables->block_tables || !tables->held || !tables->held_out || !kv_lens || !new_lens || !start_pos))
@@ -55,6 +56,8 @@ int cronus_kv_commit(const cronus_kv_cache* caches, int32_t n_caches, const int3
     if (int rc = check_cache(caches + i)) return rc;
     if (caches[i].num_kv_heads != caches->num_kv_heads || caches[i].head_dim != caches->head_dim || caches[i].kv_dtype != caches->kv_dtype)
       return CRONUS_ERR_INVALID_ARG;
+    for (int32_t j = 0; j < i; ++j)  // two wavefronts would move the same rows, one from where the other has been
+      if (caches[j].k_cache == caches[i].k_cache || caches[j].v_cache == caches[i].v_cache) return CRONUS_ERR_INVALID_ARG;
   }
   if (n_seqs < 0 || max_path < 0 || max_blocks_per_seq <= 0) return CRONUS_ERR_INVALID_ARG;
   if (n_seqs == 0) return CRONUS_OK;

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kCommitThreads) void commit_kernel(CommitParams p) 
   const int* path = p.paths + (long long)s * p.max_path;
   // The path ends at the first entry that is not one of the sequence's rows or not behind the entry before it.
   int m = 0;
-  if (start >= 0 && n > 0 && start + n <= (long long)p.max_blocks * kBlock) {
+  if (start >= 0 && n > 0 && start + n <= min((long long)p.max_blocks * kBlock, 0x7fffffffLL)) {
     const int most = min(p.path_lens[s], p.max_path);
     for (; m < most; m += 64) {
       const int k = m + lane;

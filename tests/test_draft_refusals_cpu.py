@@ -78,7 +78,7 @@ def test_build_tables_refusals():
 
 
 def commit(**kw):
-    a = dict(caches=[cache(), cache()], start=FAKE, cu=FAKE + 0x1000, paths=FAKE + 0x2000, most=4, lens=FAKE + 0x3000, bt=FAKE, width=4, n=3,
+    a = dict(caches=[cache(), cache(k=FAKE + 64, v=FAKE + 64)], start=FAKE, cu=FAKE + 0x1000, paths=FAKE + 0x2000, most=4, lens=FAKE + 0x3000, bt=FAKE, width=4, n=3,
              out=FAKE + 0x4000)
     a.update(kw)
     return B.cronus_kv_commit(a["caches"], a["start"], a["cu"], a["paths"], a["most"], a["lens"], a["bt"], a["width"], a["n"], a["out"], check=False)
@@ -95,7 +95,9 @@ def test_kv_commit_refusals():
         assert commit(caches=[cache(), cache(**kw)]) == code, kw
     for other in (dict(hkv=4), dict(d=128), dict(kv_dtype=B.CRONUS_KV_FP8_E4M3, k_scale=FAKE, v_scale=FAKE)):
         assert commit(caches=[cache(), cache(**other)]) == BAD, other
-    assert commit(caches=[cache(hq=131072, hkv=65536)] * 2) == BAD
+    assert commit(caches=[cache(hq=131072, hkv=65536)]) == BAD
+    for twice in (cache(), cache(k=FAKE + 64), cache(v=FAKE + 64)):
+        assert commit(caches=[cache(), cache(k=FAKE + 128, v=FAKE + 128), twice]) == BAD
     assert commit(n=0, start=None) == B.CRONUS_OK
     if no_gpu():
         assert commit() == B.CRONUS_ERR_HIP and commit(out=None) == B.CRONUS_ERR_HIP

@@ -165,3 +165,19 @@ def test_blocks_beyond_4_gib():
         for src, to in zip(big, s.dev_pools[0]):
             to[i * per:(i + 1) * per] = src[(blocks - 1 - i) * per:(blocks - i) * per]
     s.check()
+
+
+def test_positions_end_with_32_bits():
+    """Tables with room for 2^31 positions and more: tokens that pass them lie nowhere, those just before them move."""
+    width = 2 ** 27 + 8
+    b = State([2, 2], [6, 6], [[1, 3, 5], [0, 2]])
+    table = torch.empty(2, width, dtype=torch.int32, device=DEV)
+    table[:, :] = b.t["table"][:, :1]
+    start = np.array([2 ** 31 - 16 + 2, 2 ** 31 - 16 + 12], np.int32)
+    b.t["table"], b.t["start"], b.width = table, torch.from_numpy(start).to(DEV), width
+    b.call()
+    torch.cuda.synchronize()
+    for (k, v), (dk, dv) in zip(b.pools, b.dev_pools):  # the first as if at position 2 of its block, the second not at all
+        D.commit(k, v, b.hkv, b.d, np.array([2, -1], np.int32), b.cu, b.paths, b.path_lens, b.table)
+        assert np.array_equal(dk.cpu().numpy().view(k.dtype), k) and np.array_equal(dv.cpu().numpy().view(v.dtype), v)
+    assert b.t["out"].tolist() == [int(start[0]) + 3, int(start[1])]
