@@ -18,8 +18,12 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kMapThreads = 256, kMapTokens = 4;  // tokens of a thread of map_kernel
-constexpr int kFewTokens = 4096;                  // of a batch that plan_kernel maps, of at most kPlanThreads sequences
-constexpr int kMapSeqs = 4096;                    // sequences whose offsets map_kernel searches in LDS
+// Tokens of a batch that plan_kernel maps, of at most kPlanThreads sequences.  us a call, one launch / two: 208 tokens 6.0 / 9.0, 1024 7.8 / 8.9, 2048
+// 8.7 / 8.7, 4096 10.1 / 8.4, 16384 21.9 / 8.5.
+constexpr int kFewTokens = 2048;
+// Sequences whose offsets map_kernel searches in LDS.  us a call, there / in memory: 256 sequences, of which 64 end, 16.4 / 17.0; 512 9.4 / 10.5; 2000
+// 23.8 / 23.1; 4000 35.2 / 33.1.
+constexpr int kMapSeqs = 1024;
 
 struct TableParams {
   cronus_paged_tables t;

@@ -167,3 +167,19 @@ def test_replays_grow_the_sequences():
         s.t["kv"].copy_(torch.from_numpy(s.kv))
         s.t["new"].copy_(torch.from_numpy(s.new))
         s.t["slots"].fill_(FILL)
+
+
+@pytest.mark.parametrize("most", [1, 63, 64, 1023, 1025, 2047, 2048, 2049, 4095, 4096, 4097])
+@pytest.mark.parametrize("n", [1, 40, 1024])
+def test_batches_on_both_sides_of_a_second_launch(n, most):
+    """As many tokens as the call allows, in the sequences that have not ended; the blocks of the others are what these get."""
+    new = np.full(n, -1)
+    lives = np.arange(0, n, 2)
+    new[lives] = most // len(lives) + (np.arange(len(lives)) < most % len(lives))
+    kv = np.arange(n) % 37
+    held = -(-kv // 16)
+    need = int(np.maximum(0, -(-(kv + np.maximum(new, 0)) // 16) - held).sum())
+    back = int(held[new == -1].sum())
+    count = max(0, need - back)
+    want = State(kv, new, held, int((kv.max() + new.max()) // 16 + 1), count, count + back, most, seed=most).run()
+    assert want["status"] == 0 and want["asked"][0] == most
