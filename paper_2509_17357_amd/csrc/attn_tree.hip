@@ -15,9 +15,10 @@
 //                   joined in LDS.
 //   tiles_kernel  - row tiles of 128 or 256, bound by what a CU issues: a wavefront has 32 of the rows.  Tiles of kTileKeys keys go through registers
 //                   (fp8 codes are converted there, once) to one of two LDS buffers, where all waves read their operands.
-// What the second one is at: 16 trees of 48 .. 61 tokens, 8 heads a KV head, fp8, behind 8000 .. 32000 keys take 690 .. 710 us, 0.81 .. 0.83 PFLOP/s; the matrix pipes are busy for 41 % of it, a wave issues for 35 % and waits for LDS, memory or the barrier for 38 %, LDS moves
-// for 26 %.  Tried, within 2 % of it or slower: V and the next K read a step ahead; scores of the next sub-tile between the numerators of this one; the
-// two waves of a SIMD half a step apart; s_setprio around the products; bf16 tiles by DMA in a ring of four (204 -> 225 us, 32 trees of 64).
+// What the second one is at: 16 trees of 48 .. 61 tokens, 8 heads a KV head, fp8, behind 8000 .. 32000 keys take 690 .. 710 us, 0.81 .. 0.83 PFLOP/s; the
+// matrix pipes are busy for 40 % of it, a wave issues for 34 %, waits for its turn to for 25 % and for LDS, memory or the barrier for 41 %, LDS
+// moves for 26 %.  Tried, within 2 % of it or slower: V and the next K read a step ahead; scores of the next sub-tile between the numerators of this
+// one; the two waves of a SIMD half a step apart; s_setprio around the products; bf16 tiles by DMA in a ring of four (204 -> 225 us, 32 trees of 64).
 #include <hip/hip_runtime.h>
 #include <algorithm>
 
